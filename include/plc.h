@@ -609,6 +609,119 @@ int plc_trie_best_match(const plc_trie *trie, const int32_t *tokens, int64_t n, 
 int plc_trie_evict(plc_trie *trie, int64_t id);
 
 /*
+ * ---- Paged cache -----------------------------------------------------------------
+ * Where a decoded cache is put to work: the fp16 or bf16 rows of all sessions in pages of one pool, so that
+ * sessions that share a prefix (the one plc_trie_best_match found, the beams of a search, the branches of a
+ * draft) share its pages, and a session grows by a page and not by a copy.  The codec's calls read and write
+ * [S,L,H,n,d]; plc_pages_store and plc_pages_load move rows between that layout, or packed rows, and pages.
+ *
+ *   pool     K and V halves, logical [P, L, H, B, d] of 16-bit elements through `stride`: a page holds B
+ *            consecutive positions of one session in all layers and KV heads.
+ *   table    i32 [S, M]: entry j of session s is the page of its positions j*B .. j*B + B-1.  A session of n
+ *            positions has ceil(n / B) pages; the entries behind them are -1.
+ *   lens     i32 [S]: positions of each session.
+ *   refs     i32 [P]: number of table entries that name the page.  A page is free while it is 0.
+ * The caller fills table with -1 and lens and refs with zeros once; from then on the calls below keep them.
+ * All calls work in place and in stream order.  They raise status PLC_ERR_INVALID for lengths, page numbers or
+ * offsets that are not what is described here (the rows concerned are left alone), and never read or write
+ * outside the buffers.  What they do depends on their arguments alone, not on the order in which workgroups run:
+ * pages are taken from the lowest free number on.
+ *
+ * Rows of a call: `off` i32 [S+1], ascending from 0, gives each session t = off[s+1] - off[s] rows, which are
+ * the LAST t positions of the session, lens[s]-t .. lens[s]-1.
+ */
+typedef struct plc_pages {
+  void *k, *v;            /* 16-byte aligned                                                             */
+  int64_t stride[4];      /* element strides of (page, layer, head, row), multiples of 8; components are
+                             contiguous                                                                  */
+  int32_t P, L, H, B, d;  /* pages, layers, KV heads, rows of a page (a power of two, 16..1024), components
+                             (a multiple of 8)                                                           */
+  int32_t S, M;           /* sessions (1..1024), entries of a session                                    */
+  int32_t *table, *lens, *refs;
+} plc_pages;
+
+typedef struct plc_rows {
+  int32_t layer, layers;  /* the pool's layers layer .. layer + layers-1                                 */
+  int32_t packed;         /* 1: row x of the call is row x of the buffer, sessions one behind the other;
+                             0: row i of session s is row i of the session's part of the buffer          */
+  int64_t rows;           /* rows of the buffer (packed) or of each session's part                       */
+  int64_t stride[4];      /* element strides of (session, layer, head, row), multiples of 8; that of the
+                             session is not used with packed                                             */
+} plc_rows;
+
+/* Bytes of workspace that plc_pages_extend and plc_pages_compact need; 0 if the description is invalid.  Host call. */
+size_t plc_pages_workspace_bytes(const plc_pages *pages /* host */);
+
+/* Every session s becomes what session src[s] was before the call (beams that go on, a session that starts
+ * from another's prefix), or empty with src[s] = -1 (its pages are given back).  Pages are shared, not copied. */
+int plc_pages_fork(const plc_pages *pages, const int32_t *src, uint32_t *status, void *stream);
+
+/* Room for grow[s] >= 0 more positions of every session: the lengths grow, pages are taken.  Where the last page
+ * is begun, shared and about to be written, the session gets a copy of its rows (of all who hold it and grow in
+ * this call the one with the highest number keeps it if nobody else holds it).  If the pool has too few free pages
+ * or a session too few entries, status PLC_ERR_CAPACITY is raised and nothing changes.
+ * The new positions' rows are left as they were in the page. */
+int plc_pages_extend(const plc_pages *pages, const int32_t *grow, void *ws, size_t ws_bytes,
+                     uint32_t *status, void *stream);
+
+/* Every session keeps its first new_lens[s] <= lens[s] positions; pages behind them are given back. */
+int plc_pages_trim(const plc_pages *pages, const int32_t *new_lens, uint32_t *status, void *stream);
+
+/* Keeps the accepted nodes of a drafted tree: the session's last t positions are the tree's nodes (`off`), and
+ * path[path_off[s] .. path_off[s+1]) the numbers of those to keep, strictly ascending.  Their rows move, in all
+ * layers, to the first positions of the tree; the session ends behind them, pages that it no longer reaches are
+ * given back.  The pages that are written must be the session's own (plc_pages_extend has made them so), else
+ * status PLC_ERR_INVALID is raised and they are left alone. */
+int plc_pages_accept(const plc_pages *pages, const int32_t *off, const int32_t *path, int64_t path_len,
+                     const int32_t *path_off, uint32_t *status, void *stream);
+
+/* Moves the pages in use to the pool's front: with U pages in use, those numbered U and above go, in ascending
+ * order, to the free pages below U, in ascending order; tables and counts follow.
+ *   used   out, nullable: u32, U. */
+int plc_pages_compact(const plc_pages *pages, uint32_t *used, void *ws, size_t ws_bytes, uint32_t *status,
+                      void *stream);
+
+/* Copies rows of `k`, `v` (16-bit, addressed through `rows`) to the positions they stand for, or back.  A page that
+ * is stored to must be the session's own. */
+int plc_pages_store(const plc_pages *pages, const plc_rows *rows, const int32_t *off, const void *k,
+                    const void *v, uint32_t *status, void *stream);
+int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *off, void *k, void *v,
+                   uint32_t *status, void *stream);
+
+/*
+ * Attention of the last positions of every session over its pages, in one layer: tokens of a step, the next
+ * piece of a prompt, or a tree of drafted tokens.  With node i of session s at position c + i, c = lens[s] - t,
+ * and query head j reading KV head j / G:
+ *   score  s_p = scale * sum_e q[e] * k_p[e] over the positions p that the node sees: all p < c, itself, and its
+ *          ancestors in the tree (`parents`), or all nodes before it (parents = null: a chain);
+ *   out    sum_p exp(s_p) v_p / sum_p exp(s_p),   lse = ln sum_p exp(s_p).
+ * Products of 16-bit values accumulated in fp32, maximum and sum in fp32; the weights are rounded to the cache's
+ * type, relative to the largest so far, for the product with v.  Rows that a node does not see have no effect on
+ * it, whatever they hold.  Sessions without nodes take no part.
+ *   layer      0..L-1.
+ *   type       PLC_FP16 or PLC_BF16, of the cache, q and out.  d <= 256.
+ *   q, out     logical [N, H*G, d], element strides (node, head) in q_stride / out_stride, multiples of 8;
+ *              16-byte aligned.  Node x of the call is row x.
+ *   off        as above, off[S] <= N.
+ *   parents    nullable: i32 [N], the number within the tree of a node's parent, less than its own; -1: the node
+ *              continues the cache.
+ *   max_nodes, max_len   host: no session has more nodes, none more positions (else status PLC_ERR_INVALID is
+ *              raised and the session's rows are left alone).  They set the launch: max_len close to the longest
+ *              session's length is best.  With `parents` max_nodes <= PLC_TREE_NODES.
+ *   lse        out, nullable: fp32 [N, H*G].
+ *   ws         plc_attend_workspace_bytes(), 256-byte aligned.
+ */
+#define PLC_FP16 0
+#define PLC_BF16 1
+#define PLC_TREE_NODES 256
+size_t plc_attend_workspace_bytes(const plc_pages *pages /* host */, int32_t G, int64_t N, int32_t max_nodes,
+                                  int32_t max_len);
+int plc_attend(const plc_pages *pages, int32_t layer, int32_t type, const void *q, const int64_t *q_stride /* host */,
+               int32_t G, int64_t N, const int32_t *off, const int32_t *parents, int32_t max_nodes,
+               int32_t max_len, float scale, void *out, const int64_t *out_stride /* host */, float *lse,
+               void *ws, size_t ws_bytes, uint32_t *status, void *stream);
+
+/*
  * Instrumentation for benchmarks (not part of the coding path; process-wide,
  * not thread-safe).  While a pair of hipEvent_t (passed as void*) is set for
  * a kernel id, each later call records `start` immediately before and `stop`

@@ -19,7 +19,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libplc.so")
 HIP_SOURCES = ["plc_api.hip", "plc_predict.hip", "plc_hist_freq.hip", "plc_rans.hip", "plc_index.hip",
-               "plc_linear.hip"]
+               "plc_linear.hip", "plc_pages.hip", "plc_attend.hip"]
 CXX_SOURCES = ["plc_trie.cpp"]
 COMMON = ["-O3", "-std=c++17", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # The coders read and write their LDS stages and packed rows through pointers of several types; the order of

@@ -35,10 +35,14 @@ EXPORTS = ("plc_version", "plc_strerror", "plc_workspace_bytes", "plc_units_per_
            "plc_rans_decode_reconstruct_restart", "plc_rans_decode_reconstruct_cond_restart",
            "plc_rans_decode_reconstruct_adapt_restart",
            "plc_expected_embedding", "plc_predict_residual_linear", "plc_reconstruct_linear",
+           "plc_pages_workspace_bytes", "plc_pages_fork", "plc_pages_extend", "plc_pages_trim", "plc_pages_accept",
+           "plc_pages_compact", "plc_pages_store", "plc_pages_load", "plc_attend_workspace_bytes", "plc_attend",
            "plc_trie_create", "plc_trie_destroy", "plc_trie_size", "plc_trie_nodes", "plc_trie_insert",
            "plc_trie_best_match", "plc_trie_evict")
 
 MAX_BITS = 4
+PLC_FP16, PLC_BF16 = 0, 1
+TREE_NODES = 256
 RESTART_WORDS = 34
 
 (TRACE_PREDICT, TRACE_RECONSTRUCT, TRACE_HISTOGRAM, TRACE_RANS_ENCODE, TRACE_RANS_DECODE,
@@ -61,6 +65,18 @@ class plc_dims(C.Structure):
 
 class plc_restart(C.Structure):
     _fields_ = [("points", C.c_void_p), ("scratch", C.c_void_p), ("per_stream", C.c_int32)]
+
+
+class plc_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride", C.c_int64 * 4),
+                ("P", C.c_int32), ("L", C.c_int32), ("H", C.c_int32), ("B", C.c_int32), ("d", C.c_int32),
+                ("S", C.c_int32), ("M", C.c_int32),
+                ("table", C.c_void_p), ("lens", C.c_void_p), ("refs", C.c_void_p)]
+
+
+class plc_rows(C.Structure):
+    _fields_ = [("layer", C.c_int32), ("layers", C.c_int32), ("packed", C.c_int32), ("rows", C.c_int64),
+                ("stride", C.c_int64 * 4)]
 
 
 _lib = None
@@ -129,6 +145,19 @@ def lib() -> C.CDLL:
                                                                p, p, p, sz, rp, p, p]
         L.plc_rans_decode_reconstruct_adapt_restart.argtypes = [dp, p, p, p, u64, p, p, i32, i32, p, p, p, p, p,
                                                                 C.c_float, p, u64, p, p, p, p, p, sz, rp, p, p]
+        gp, kp, i64s = C.POINTER(plc_pages), C.POINTER(plc_rows), C.POINTER(i64)
+        L.plc_pages_workspace_bytes.restype = sz
+        L.plc_pages_workspace_bytes.argtypes = [gp]
+        L.plc_pages_fork.argtypes = [gp, p, p, p]
+        L.plc_pages_extend.argtypes = [gp, p, p, sz, p, p]
+        L.plc_pages_trim.argtypes = [gp, p, p, p]
+        L.plc_pages_accept.argtypes = [gp, p, p, i64, p, p, p]
+        L.plc_pages_compact.argtypes = [gp, p, p, sz, p, p]
+        L.plc_pages_store.argtypes = [gp, kp, p, p, p, p, p]
+        L.plc_pages_load.argtypes = [gp, kp, p, p, p, p, p]
+        L.plc_attend_workspace_bytes.restype = sz
+        L.plc_attend_workspace_bytes.argtypes = [gp, i32, i64, i32, i32]
+        L.plc_attend.argtypes = [gp, i32, i32, p, i64s, i32, i64, p, p, i32, i32, C.c_float, p, i64s, p, p, sz, p, p]
         L.plc_trie_create.restype = p
         L.plc_trie_create.argtypes = [C.c_double]
         L.plc_trie_destroy.restype = None
@@ -495,6 +524,106 @@ def plc_reconstruct_linear(dims, ebar, A, bias_k, bias_v, symbols, esc_vals, esc
         _contig(esc_off, torch.int64), _ptr(out_k, torch.float16), _ptr(out_v, torch.float16),
         _contig(ws, torch.uint8), ws.numel(), _contig(status, torch.int32), _stream())
     _check(rc, "plc_reconstruct_linear")
+
+
+def make_pages(k, v, table, lens, refs) -> plc_pages:
+    """k, v [P, L, H, B, d] of 16-bit elements (same strides, components contiguous); table int32 [S, M]; lens int32 [S];
+    refs int32 [P].  The tensors have to outlive what is made here."""
+    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(4) != 1:
+        raise ValueError("k and v are [pages, layers, heads, rows, components] of one shape, type and layout")
+    if k.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"expected float16 or bfloat16, got {k.dtype}")
+    if table.dim() != 2 or lens.shape != table.shape[:1] or refs.shape != k.shape[:1]:
+        raise ValueError("table [sessions, entries], lens [sessions], refs [pages]")
+    pages = plc_pages()
+    pages.k, pages.v = _ptr(k), _ptr(v)
+    pages.stride = (C.c_int64 * 4)(*k.stride()[:4])
+    pages.P, pages.L, pages.H, pages.B, pages.d = k.shape
+    pages.S, pages.M = table.shape
+    pages.table, pages.lens, pages.refs = (_contig(t, torch.int32) for t in (table, lens, refs))
+    return pages
+
+
+def plc_pages_workspace_bytes(pages) -> int:
+    return int(lib().plc_pages_workspace_bytes(C.byref(pages)))
+
+
+def plc_pages_fork(pages, src, status):
+    """src int32 [S]: what each session becomes; -1: empty."""
+    rc = lib().plc_pages_fork(C.byref(pages), _contig(src, torch.int32), _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_fork")
+
+
+def plc_pages_extend(pages, grow, ws, status):
+    rc = lib().plc_pages_extend(C.byref(pages), _contig(grow, torch.int32), _contig(ws, torch.uint8), ws.numel(),
+                                _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_extend")
+
+
+def plc_pages_trim(pages, new_lens, status):
+    rc = lib().plc_pages_trim(C.byref(pages), _contig(new_lens, torch.int32), _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_trim")
+
+
+def plc_pages_accept(pages, off, path, path_off, status):
+    """off, path_off int32 [S+1]; path int32: numbers of the nodes to keep, ascending in each session."""
+    rc = lib().plc_pages_accept(C.byref(pages), _contig(off, torch.int32), _contig(path, torch.int32), path.numel(),
+                                _contig(path_off, torch.int32), _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_accept")
+
+
+def plc_pages_compact(pages, used, ws, status):
+    """used int32 [1] out, or None: pages in use."""
+    rc = lib().plc_pages_compact(C.byref(pages), _contig(used, torch.int32), _contig(ws, torch.uint8), ws.numel(),
+                                 _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_compact")
+
+
+def _rows_of(k, v, layer):
+    """Rows in a buffer: packed [rows, layers, heads, d], or [S, layers, heads, rows, d], of any strides but the last."""
+    if k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(-1) != 1 or k.dim() not in (4, 5):
+        raise ValueError("k and v are [rows, layers, heads, d] or [sessions, layers, heads, rows, d] of one layout")
+    r = plc_rows()
+    r.packed = int(k.dim() == 4)
+    r.layer, r.layers, r.rows = layer, k.shape[1], k.shape[0] if r.packed else k.shape[3]
+    st = k.stride()
+    r.stride = (C.c_int64 * 4)(0, st[1], st[2], st[0]) if r.packed else (C.c_int64 * 4)(*st[:4])
+    return r
+
+
+def plc_pages_store(pages, off, k, v, layer, status):
+    """k, v [rows, layers, H, d] packed, or [S, layers, H, rows, d]; off int32 [S+1]; layer: the first of the pool's."""
+    rc = lib().plc_pages_store(C.byref(pages), C.byref(_rows_of(k, v, layer)), _contig(off, torch.int32), _ptr(k), _ptr(v),
+                               _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_store")
+
+
+def plc_pages_load(pages, off, k, v, layer, status):
+    """plc_pages_store the other way round."""
+    rc = lib().plc_pages_load(C.byref(pages), C.byref(_rows_of(k, v, layer)), _contig(off, torch.int32), _ptr(k), _ptr(v),
+                              _contig(status, torch.int32), _stream())
+    _check(rc, "plc_pages_load")
+
+
+def plc_attend_workspace_bytes(pages, G, N, max_nodes, max_len) -> int:
+    return int(lib().plc_attend_workspace_bytes(C.byref(pages), int(G), int(N), int(max_nodes), int(max_len)))
+
+
+def plc_attend(pages, layer, q, off, parents, max_nodes, max_len, scale, out, lse, ws, status):
+    """q, out [N, H*G, d], components contiguous; parents int32 [N] or None (a chain); lse float32 [N, H*G] or None."""
+    if q.shape != out.shape or q.dtype != out.dtype or q.dim() != 3 or q.stride(2) != 1 or out.stride(2) != 1:
+        raise ValueError("q and out are [nodes, heads, d] of one type, with contiguous components")
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"expected float16 or bfloat16, got {q.dtype}")
+    if q.shape[1] % pages.H or q.shape[2] != pages.d:
+        raise ValueError("query heads are a multiple of the cache's, with as many components")
+    qs, os_ = q.stride(), out.stride()
+    rc = lib().plc_attend(C.byref(pages), layer, PLC_FP16 if q.dtype == torch.float16 else PLC_BF16, _ptr(q),
+                          (C.c_int64 * 2)(qs[0], qs[1]), q.shape[1] // pages.H, q.shape[0], _contig(off, torch.int32),
+                          _contig(parents, torch.int32), max_nodes, max_len, scale, _ptr(out),
+                          (C.c_int64 * 2)(os_[0], os_[1]), _contig(lse, torch.float32), _contig(ws, torch.uint8), ws.numel(),
+                          _contig(status, torch.int32), _stream())
+    _check(rc, "plc_attend")
 
 
 class PrefixTrie:

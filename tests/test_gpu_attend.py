@@ -1,0 +1,345 @@
+"""plc_attend against the formula in 64 bits, over the shapes, trees and values where it can go wrong."""
+import math
+import random
+
+import pytest
+import torch
+
+from paper_2604_15356_amd import plc
+from paper_2604_15356_amd.paged import PagedKVCache
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def offsets(counts):
+    return ints([sum(counts[:i]) for i in range(len(counts) + 1)])
+
+
+def random_tree(rng, t):
+    return [rng.randrange(max(-1, i - 9), i) for i in range(t)]
+
+
+def make(dtype, d, H, B, lens, seed, L=1, layout="plain", fill=float("nan")):
+    """A cache with these lengths, on pages in random order; rows that no session has hold `fill`."""
+    rng = random.Random(seed)
+    torch.manual_seed(seed)
+    counts = [-(-n // B) for n in lens]
+    P, M = sum(counts) + 3, max(counts) + 1
+    if layout == "plain":
+        k, v = (torch.full((P, L, H, B, d), fill, dtype=dtype, device=DEV) for _ in range(2))
+    else:  # rows of all heads next to each other, components with a gap behind
+        k, v = (torch.full((P, L, B, H, d + 8), fill, dtype=dtype, device=DEV)[..., :d].permute(0, 1, 3, 2, 4) for _ in range(2))
+    free = rng.sample(range(P), P)
+    table = [[free.pop() for _ in range(c)] for c in counts]
+    refs = torch.zeros(P, dtype=torch.int32, device=DEV)
+    refs[ints([p for row in table for p in row]).long()] = 1
+    cache = PagedKVCache(k, v, ints([row + [-1] * (M - len(row)) for row in table]), ints(lens), refs)
+    rows = [torch.randn((sum(lens), L, H, d), device=DEV).to(dtype) for _ in range(2)]
+    if sum(lens):
+        cache.store(*rows, offsets(lens))
+    cache.check_status()
+    return cache, rows
+
+
+def definition(q, k, v, lens, counts, parents, G, scale):
+    """(out, lse, sum of weights times |v|, largest sum |q k|) in 64 bits; k, v [rows, H, d] packed over the sessions.
+    Positions that a node does not see take no part, whatever they hold."""
+    N, heads, d = q.shape
+    H = heads // G
+    out, absolute = (torch.zeros((N, heads, d), dtype=torch.float64) for _ in range(2))
+    lse = torch.full((N, heads), -math.inf, dtype=torch.float64)
+    size = torch.zeros((N, heads), dtype=torch.float64)
+    q, k, v = (x.double().cpu() for x in (q, k, v))
+    row0 = x = 0
+    for n, t in zip(lens, counts):
+        for i in range(t):
+            seen, a = list(range(n - t)), i
+            while a >= 0:
+                seen.append(n - t + a)
+                a = parents[x - i + a] if parents is not None else a - 1
+            seen = torch.tensor(seen) + row0
+            for h in range(H):
+                qs, ks, vs = q[x, h * G:(h + 1) * G], k[seen, h], v[seen, h]
+                s = scale * (qs @ ks.T)
+                lse[x, h * G:(h + 1) * G] = torch.logsumexp(s, 1)
+                w = torch.softmax(s, 1)
+                out[x, h * G:(h + 1) * G] = w @ vs
+                absolute[x, h * G:(h + 1) * G] = w @ vs.abs()
+                size[x, h * G:(h + 1) * G] = (scale * (qs.abs() @ ks.abs().T)).amax(1)
+            x += 1
+        row0 += n
+    return out, lse, absolute, size
+
+
+def bounds(dtype, d, n, out, lse, absolute, size, vmax):
+    """How far a right result can be off, from the roundings: a score's products are exact in 32 bits and their sum of d has
+    d additions; multiplying by the scale, the subtraction of the maximum and exp2 add a few; a weight is then off by the
+    score's error, relatively, and by half a step of its type; the sums of n weights and of n products add up to n + 2 more
+    roundings in 32 bits each (joins of chunks included); the result is rounded once.  Weights far below 1 are held in steps
+    of 2^-24 in fp16 (its smallest), of nothing that matters in bf16."""
+    half = torch.finfo(dtype).eps / 2
+    u = 2.0 ** -24
+    score = size * (d + 4) * u + (lse.abs() + size) * 4 * u + 8 * u
+    weight = 2 * score + 2 * (n + 4) * u
+    tol = (half * 1.01 + weight)[..., None] * absolute + half * 1.01 * out.abs()
+    if dtype == torch.float16:
+        tol = tol + n * 2.0 ** -25 * vmax + 2.0 ** -25
+    else:
+        tol = tol + 1e-30
+    return tol, score + (n + 4) * u
+
+
+def check(dtype, d, G, H, B, lens, counts, tree, seed, layout="plain", scale=None, L=1, layer=0, hints=True, sharp=1.0):
+    rng = random.Random(seed)
+    cache, (k, v) = make(dtype, d, H, B, lens, seed, L=L, layout=layout)
+    N = sum(counts)
+    q = (sharp * torch.randn((N, H * G, d + (8 if layout != "plain" else 0)), device=DEV)).to(dtype)[..., :d]
+    parents = [p for t in counts for p in random_tree(rng, t)] if tree else None
+    kw = dict(max_nodes=max(counts + [1]), max_len=max(lens + [1])) if hints else {}
+    got, lse = cache.attend(q, offsets(counts), parents=None if parents is None else ints(parents), layer=layer, scale=scale, **kw)
+    cache.check_status()
+    scale = d ** -0.5 if scale is None else scale
+    want, want_lse, absolute, size = definition(q, k[:, layer], v[:, layer], lens, counts, parents, G, scale)
+    tol, tol_lse = bounds(dtype, d, max(lens), want, want_lse, absolute, size, float(v.abs().max()) if v.numel() else 0)
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
+    off = (lse.double().cpu() - want_lse).abs()
+    assert bool((off <= tol_lse).all()), float((off / tol_lse).max())
+    return cache, q, parents, got, lse
+
+
+BOTH = pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+
+
+@BOTH
+@pytest.mark.parametrize("d", [8, 40, 64, 80, 128, 136, 256])
+@pytest.mark.parametrize("G,t", [(1, 1), (3, 7), (4, 12), (5, 33)])
+def test_components_and_rows(dtype, d, G, t):
+    """Every width of the kernels, whole and not, with rows for each of their arrangements."""
+    check(dtype, d, G, 2, 16, [t + 100, t], [t, t], True, seed=d + t)
+
+
+@BOTH
+@pytest.mark.parametrize("lens,counts", [([1], [1]), ([2, 1, 3], [1, 1, 1]), ([16, 17, 15, 31, 32, 33], [1] * 6),
+                                         ([127, 128, 129, 300], [1] * 4), ([5, 0, 40, 9], [5, 0, 0, 2]), ([1000, 257], [1, 3])])
+@pytest.mark.parametrize("B", [16, 64])
+def test_lengths(dtype, lens, counts, B):
+    check(dtype, 64, 2, 2, B, lens, counts, False, seed=len(lens) + B)
+
+
+@BOTH
+@pytest.mark.parametrize("t", [2, 63, 64, 65, 130, 256])
+def test_trees_across_the_words_of_their_masks(dtype, t):
+    check(dtype, 64, 1, 2, 32, [t + 45, t], [t, t], True, seed=t)
+
+
+@pytest.mark.parametrize("t,n", [(17, 17), (100, 333), (300, 300), (513, 700)])
+def test_chains_of_a_prompts_pieces(t, n):
+    check(torch.bfloat16, 128, 2, 1, 16, [n, 40], [t, 40], False, seed=t)
+
+
+@BOTH
+@pytest.mark.parametrize("n", [5000, 20011])
+@pytest.mark.parametrize("t,G", [(1, 4), (9, 4), (40, 4)])
+def test_long_contexts_are_joined_from_chunks(dtype, n, t, G):
+    check(dtype, 128, G, 1, 16, [n, 700, t], [t, t, t], True, seed=n + t)
+
+
+def test_strides_layers_and_scales():
+    for layer in range(3):
+        check(torch.float16, 80, 2, 3, 16, [50, 7], [5, 7], True, seed=layer, layout="gaps", L=3, layer=layer, scale=0.3)
+    check(torch.bfloat16, 128, 4, 2, 1024, [1500, 3], [2, 1], False, seed=9, hints=False)
+
+
+def test_sharp_scores():
+    """Scores of a hundred and more: the maximum moves by leaps, most weights vanish."""
+    for dtype in (torch.float16, torch.bfloat16):
+        check(dtype, 64, 2, 2, 16, [900, 70], [4, 4], True, seed=3, sharp=30.0)
+
+
+@BOTH
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_what_a_node_does_not_see_has_no_effect(dtype, bad):
+    """Infinities and NaN in the rows of other branches, and behind the end: the results are those without, bit for bit."""
+    t, n, d, H, G, B = 30, 75, 64, 2, 2, 16
+    for rows_per in (1, 8):
+        cache, (k, v) = make(dtype, d, H, B, [n], seed=4, fill=bad)
+        G = rows_per
+        q = torch.randn((t, H * G, d), device=DEV).to(dtype)
+        parents = [-1 if i % 2 == 0 and i < 4 else i - 2 if i >= 2 else -1 for i in range(t)]  # even and odd branches
+        clean, clean_lse = cache.attend(q, offsets([t]), parents=ints(parents))
+        odd = torch.zeros(n, dtype=torch.bool, device=DEV)
+        odd[n - t + 1:: 2] = True
+        k2, v2 = k.clone(), v.clone()
+        k2[odd], v2[odd, :, :, ::3] = bad, bad
+        cache.store(k2, v2, offsets([n]))
+        got, lse = cache.attend(q, offsets([t]), parents=ints(parents))
+        cache.check_status()
+        assert torch.isfinite(clean).all() and torch.equal(got[::2], clean[::2]) and torch.equal(lse[::2], clean_lse[::2])
+        if bad != bad:
+            assert torch.isnan(got[1::2][..., ::3]).all() and torch.isnan(lse[1::2]).all()
+
+
+@BOTH
+def test_infinite_values_that_are_seen(dtype):
+    """Of V, in the context and in the tree: the components they are in come out infinite, the others as ever."""
+    t, n, d = 6, 70, 64
+    cache, (k, v) = make(dtype, d, 1, 16, [n], seed=6)
+    q = torch.randn((t, 1, d), device=DEV).to(dtype)
+    parents = [-1, 0, 1, -1, 3, 4]
+    clean, _ = cache.attend(q, offsets([t]), parents=ints(parents))
+    v2 = v.clone()
+    v2[3, 0, 0, 5] = math.inf      # everybody sees it
+    v2[n - t + 1, 0, 0, 9] = -math.inf  # nodes 1 and 2 see it
+    cache.store(k, v2, offsets([n]))
+    got, _ = cache.attend(q, offsets([t]), parents=ints(parents))
+    cache.check_status()
+    assert (got[:, 0, 5] == math.inf).all() and (got[1:3, 0, 9] == -math.inf).all()
+    rest = torch.ones((t, d), dtype=torch.bool, device=DEV)
+    rest[:, 5] = False
+    rest[1:3, 9] = False
+    assert torch.equal(got[:, 0][rest], clean[:, 0][rest])
+
+
+def test_scores_of_the_lowest_value():
+    """Rows of which nothing is left but the lowest scores: zeros, and a sum of minus infinity."""
+    cache, (k, v) = make(torch.bfloat16, 64, 1, 16, [40], seed=8)
+    q = torch.zeros((2, 1, 64), device=DEV, dtype=torch.bfloat16)
+    q[0] = 1.0
+    k2 = torch.full_like(k, -math.inf)
+    cache.store(k2, v, offsets([40]))
+    got, lse = cache.attend(q[:1], offsets([1]))
+    assert (got == 0).all() and (lse == -math.inf).all()
+    k2.fill_(torch.finfo(torch.bfloat16).min)  # as far down as fp32 goes: equal weights, or none
+    cache.store(k2, v, offsets([40]))
+    got, lse = cache.attend(q[:1] * 0 + 2.0 ** -120, offsets([1]))
+    cache.check_status()
+    want = v[:, 0, 0].double().mean(0)
+    assert torch.allclose(got[0, 0].double(), want, atol=2.0 ** -8 * float(v.abs().max()))
+    cache.check_status()
+
+
+def test_broken_descriptions_raise_status():
+    def refused(call):
+        cache, _ = make(torch.float16, 64, 1, 16, [40, 30], seed=2)
+        q = torch.randn((6, 2, 64), device=DEV, dtype=torch.float16)
+        out = torch.full_like(q, 5.0)
+        call(cache, q, out)
+        with pytest.raises(plc.PlcError) as e:
+            cache.check_status()
+        assert e.value.code == plc.PLC_ERR_INVALID
+        return out
+
+    three = offsets([3, 3])
+    refused(lambda c, q, o: c.attend(q, three, parents=ints([-1, 1, 0, -1, 0, 1]), out=o))  # a node that is its own parent
+    refused(lambda c, q, o: c.attend(q, three, parents=ints([-1, 0, 2, -1, 0, 1]), out=o))
+    refused(lambda c, q, o: c.attend(q, three, parents=ints([-2, 0, 1, -1, 0, 1]), out=o))
+    out = refused(lambda c, q, o: c.attend(q, three, max_nodes=2, out=o))
+    assert (out == 5).all()
+    out = refused(lambda c, q, o: c.attend(q, three, max_len=39, out=o))
+    assert (out[:3] == 5).all() and not (out[3:] == 5).any()
+    for off in ([0, 3, 7], [-1, 3, 6], [0, 3, 2]):
+        refused(lambda c, q, o: c.attend(q, ints(off), out=o))
+    for page in (-1, 100, 2**31 - 1, -2**31):
+        def broken(c, q, o):
+            c.table[0, 1] = page
+            c.attend(q, three, out=o)
+        refused(broken)
+    for length in (-1, 2, 65, 2**31 - 1):
+        def broken(c, q, o):
+            c.lens[0] = length
+            c.attend(q, three, out=o)
+        refused(broken)
+
+
+def test_another_stream_and_a_graph():
+    """A step on a stream of its own, eagerly and captured, gives the same as on the default one, at every replay."""
+    torch.manual_seed(1)
+    S, L, H, G, d, B, t = 3, 2, 2, 4, 64, 16, 5
+    start = [40, 16, 3]
+    counts, path, path_off = [t] * S, ints([0, 2, 1, 3, 4, 0]), offsets([2, 3, 1])
+    parents = ints([-1, 0, 0, 2, -1] * S)
+    k, v = (torch.randn((S * t, L, H, d), device=DEV, dtype=torch.float16) for _ in range(2))
+    q = torch.randn((S * t, H * G, d), device=DEV, dtype=torch.float16)
+    off, grow, src = offsets(counts), ints(counts), ints([0, 1, 1])
+    cache, _ = make(torch.float16, d, H, B, start, seed=1, L=L, fill=0.0)
+    state = (cache.k, cache.v, cache.table, cache.lens, cache.refs)
+    before = [x.clone() for x in state]
+    cache.reserve(G, S * t, t, 4 * B)
+    outs = [torch.zeros_like(q) for _ in range(L)]
+
+    def step():
+        cache.fork(src)
+        cache.extend(grow)
+        cache.store(k, v, off)
+        for layer in range(L):
+            cache.attend(q, off, parents=parents, layer=layer, max_nodes=t, max_len=4 * B, out=outs[layer])
+        cache.accept(off, path, path_off)
+        cache.compact()
+
+    def rewind():
+        for x, b in zip(state, before):
+            x.copy_(b)
+
+    step()
+    cache.check_status()
+    want = [x.clone() for x in outs + list(state)]
+    side = torch.cuda.Stream()
+    rewind()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for x in outs:
+            x.zero_()
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(outs + list(state), want))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        rewind()
+        for x in outs:
+            x.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(outs + list(state), want))
+        cache.check_status()
+    many, off = torch.zeros((400, H * G, d), dtype=torch.float16, device=DEV), ints([0, 400, 400, 400])
+    with pytest.raises(RuntimeError, match="reserve"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            cache.attend(many, off, max_len=1 << 20)
+
+
+def test_no_nodes():
+    cache, _ = make(torch.float16, 64, 1, 16, [40], seed=2)
+    out, lse = cache.attend(torch.zeros((0, 2, 64), dtype=torch.float16, device=DEV), offsets([0]))
+    assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
+    cache.check_status()
+
+
+def test_a_cache_beyond_32_bits():
+    """Rows on pages whose elements lie beyond 2^31, and a page that every session shares."""
+    H, B, d, G = 2, 1024, 128, 2
+    P = (1 << 31) // (H * B * d) + 4
+    k, v = (torch.empty((P, 1, H, B, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    pages = [P - 1, 0, P - 2]
+    torch.manual_seed(3)
+    for p in pages:
+        k[p], v[p] = (torch.randn((1, H, B, d), device=DEV).to(torch.bfloat16) for _ in range(2))
+    refs = torch.zeros(P, dtype=torch.int32, device=DEV)
+    cache = PagedKVCache(k, v, ints([pages, pages]), ints([3 * B - 5, B + 1]), refs)
+    q = torch.randn((4, H * G, d), device=DEV).to(torch.bfloat16)
+    got, lse = cache.attend(q, offsets([3, 1]), parents=ints([-1, -1, 0, -1]))
+    cache.check_status()
+    rows = [torch.cat([x[p, 0].transpose(0, 1) for p in pages]) for x in (k, v)]
+    lens = [3 * B - 5, B + 1]
+    packed = [torch.cat([x[:n] for n in lens]) for x in rows]
+    want, want_lse, absolute, size = definition(q, *packed, lens, [3, 1], [-1, -1, 0, -1], G, d ** -0.5)
+    tol, tol_lse = bounds(torch.bfloat16, d, 3 * B, want, want_lse, absolute, size, 0)
+    assert bool(((got.double().cpu() - want).abs() <= tol).all()) and bool(((lse.double().cpu() - want_lse).abs() <= tol_lse).all())

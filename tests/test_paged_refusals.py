@@ -1,0 +1,137 @@
+"""What the paged cache's calls refuse on the host, before anything is enqueued: no GPU is needed, and no pointer here is
+one."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2604_15356_amd import plc
+
+P = C.c_void_p(4096)
+ODD = C.c_void_p(4098)
+
+
+def _pages(**over):
+    g = plc.plc_pages()
+    g.k = g.v = 4096
+    g.P, g.L, g.H, g.B, g.d, g.S, g.M = 10, 2, 2, 16, 64, 3, 4
+    g.stride = (C.c_int64 * 4)(2 * 2 * 16 * 64, 2 * 16 * 64, 16 * 64, 64)
+    g.table = g.lens = g.refs = 4096
+    for name, value in over.items():
+        if name.startswith("stride"):
+            g.stride[int(name[6:])] = value
+        else:
+            setattr(g, name, value)
+    return g
+
+
+def _rows(**over):
+    r = plc.plc_rows()
+    r.layer, r.layers, r.packed, r.rows = 0, 2, 1, 5
+    r.stride = (C.c_int64 * 4)(0, 128, 64, 256)
+    for name, value in over.items():
+        if name.startswith("stride"):
+            r.stride[int(name[6:])] = value
+        else:
+            setattr(r, name, value)
+    return r
+
+
+BIG = 1 << 24
+
+
+def _calls(g):
+    L, b, r = plc.lib(), C.byref(g), C.byref(_rows())
+    st = (C.c_int64 * 2)(8 * 64, 64)
+    return [L.plc_pages_fork(b, P, P, None), L.plc_pages_extend(b, P, P, BIG, P, None), L.plc_pages_trim(b, P, P, None),
+            L.plc_pages_accept(b, P, P, 5, P, P, None), L.plc_pages_compact(b, P, P, BIG, P, None),
+            L.plc_pages_store(b, r, P, P, P, P, None), L.plc_pages_load(b, r, P, P, P, P, None),
+            L.plc_attend(b, 0, 0, P, st, 2, 5, P, None, 5, 64, 1.0, P, st, P, P, BIG, P, None)]
+
+
+@pytest.mark.parametrize("over", [
+    dict(k=None), dict(v=4104), dict(table=None), dict(lens=4098), dict(refs=None), dict(P=0), dict(L=0), dict(H=-1),
+    dict(B=8), dict(B=24), dict(B=2048), dict(d=0), dict(d=12), dict(S=0), dict(S=1025), dict(M=0), dict(M=1 << 27),
+    dict(stride0=4), dict(stride1=-8), dict(stride2=12), dict(stride3=56), dict(stride3=1 << 27), dict(L=1 << 14, H=1 << 14)])
+def test_descriptions_that_are_refused(over):
+    g = _pages(**over)
+    assert plc.plc_pages_workspace_bytes(g) == 0
+    assert plc.plc_attend_workspace_bytes(g, 2, 5, 5, 64) == 0
+    assert _calls(g) == [plc.PLC_ERR_INVALID] * 8
+    assert plc.lib().plc_pages_fork(None, P, P, None) == plc.PLC_ERR_INVALID
+
+
+def test_arguments_that_are_refused():
+    L, g = plc.lib(), _pages()
+    b, st = C.byref(g), (C.c_int64 * 2)(8 * 64, 64)
+    assert plc.plc_pages_workspace_bytes(g) % 256 == 0 and plc.plc_pages_workspace_bytes(g) >= 4 * 3 * 10
+    bad = plc.PLC_ERR_INVALID
+    assert L.plc_pages_fork(b, None, P, None) == bad and L.plc_pages_fork(b, ODD, P, None) == bad
+    assert L.plc_pages_fork(b, P, None, None) == bad
+    assert L.plc_pages_extend(b, None, P, BIG, P, None) == bad
+    assert L.plc_pages_extend(b, P, P, 16, P, None) == bad and L.plc_pages_extend(b, P, ODD, BIG, P, None) == bad
+    assert L.plc_pages_extend(b, P, P, BIG, None, None) == bad
+    assert L.plc_pages_trim(b, None, P, None) == bad and L.plc_pages_trim(b, P, None, None) == bad
+    for hole in (1, 2, 4, 5):
+        args = [b, P, P, 5, P, P, None]
+        args[hole] = None
+        assert L.plc_pages_accept(*args) == bad, hole
+    assert L.plc_pages_accept(b, P, P, -1, P, P, None) == bad
+    assert L.plc_pages_compact(b, P, P, 16, P, None) == bad and L.plc_pages_compact(b, P, None, BIG, P, None) == bad
+    assert L.plc_pages_compact(b, P, P, BIG, None, None) == bad
+    for call in (L.plc_pages_store, L.plc_pages_load):
+        for over in (dict(layer=-1), dict(layer=1), dict(layers=0), dict(layers=3), dict(packed=2), dict(rows=-1),
+                     dict(rows=1 << 31), dict(stride1=4), dict(stride2=-8), dict(stride3=1), dict(packed=0, stride0=4)):
+            assert call(b, C.byref(_rows(**over)), P, P, P, P, None) == bad, over
+        for hole in (1, 2, 3, 4, 5):
+            args = [b, C.byref(_rows()), P, P, P, P, None]
+            args[hole] = None
+            assert call(*args) == bad, hole
+        assert call(b, C.byref(_rows()), P, C.c_void_p(4104), P, P, None) == bad
+        assert call(b, C.byref(_rows(rows=0)), P, P, P, P, None) == plc.PLC_OK  # nothing to move: nothing is enqueued
+
+    def attend(**over):
+        a = dict(pages=b, layer=0, type=0, q=P, qs=st, G=2, N=5, off=P, parents=None, nodes=5, len=64, scale=1.0, out=P, os=st,
+                 lse=P, ws=P, bytes=BIG, status=P)
+        a.update(over)
+        return L.plc_attend(*a.values(), None)
+
+    odd_strides = (C.c_int64 * 2)(8 * 64, 60)
+    for over in (dict(layer=-1), dict(layer=2), dict(type=2), dict(q=None), dict(q=C.c_void_p(4104)), dict(qs=None),
+                 dict(qs=odd_strides), dict(os=odd_strides), dict(os=None), dict(G=0), dict(G=1 << 16), dict(N=-1),
+                 dict(N=1 << 31), dict(off=None), dict(off=ODD), dict(parents=ODD), dict(parents=P, nodes=257), dict(nodes=0),
+                 dict(nodes=1 << 30), dict(len=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+                 dict(scale=float("inf")), dict(out=None), dict(lse=ODD), dict(ws=None), dict(ws=C.c_void_p(4096 + 128)),
+                 dict(len=1 << 20, bytes=256), dict(status=None)):
+        assert attend(**over) == bad, over
+    assert attend(N=0) == plc.PLC_OK
+    assert L.plc_attend(C.byref(_pages(d=264, stride3=264)), 0, 0, P, st, 2, 5, P, None, 5, 64, 1.0, P, st, P, P, BIG, P,
+                        None) == bad
+    # the workspace: the partial results of every chunk but where there is one
+    assert plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 64) == 256
+    assert plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 1 << 20) >= 2 * 5 * 4 * 66 * 4
+
+
+def test_tensors_that_the_binding_refuses():
+    k = torch.zeros(4, 2, 2, 16, 64, dtype=torch.float16)
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="device tensors"):
+        plc.make_pages(k, k, ints(3, 2), ints(3), ints(4))
+    for args in ((k, k[:, :1], ints(3, 2), ints(3), ints(4)), (k, k.transpose(3, 4), ints(3, 2), ints(3), ints(4)),
+                 (k[0], k[0], ints(3, 2), ints(3), ints(4)), (k, k, ints(3, 2), ints(2), ints(4)),
+                 (k, k, ints(3, 2), ints(3), ints(5))):
+        with pytest.raises(ValueError):
+            plc.make_pages(*args)
+    with pytest.raises(TypeError):
+        plc.make_pages(k.float(), k.float(), ints(3, 2), ints(3), ints(4))
+    g, rows = _pages(), torch.zeros(5, 2, 2, 64, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        plc.plc_pages_store(g, ints(4), rows, rows[:4], 0, ints(1))
+    with pytest.raises(ValueError):
+        plc.plc_pages_load(g, ints(4), rows[0], rows[0], 0, ints(1))
+    q = torch.zeros(5, 4, 64, dtype=torch.float16)
+    for bad_q in (q[:, :3], q[:, :, :32], q.permute(0, 2, 1)):
+        with pytest.raises(ValueError):
+            plc.plc_attend(g, 0, bad_q, ints(4), None, 5, 64, 1.0, bad_q, None, ints(256), ints(1))
+    with pytest.raises(TypeError):
+        plc.plc_attend(g, 0, q.float(), ints(4), None, 5, 64, 1.0, q.float(), None, ints(256), ints(1))
