@@ -8,15 +8,24 @@
 // accumulators' positions 8 a + 4 h + b (lane half h, a, b = 0..3) taken as the order of the product's inner index, V^T has
 // to come in that same order, which two transposing LDS reads of 4 positions x 16 components give.
 //
-// Positions are cut into chunks, one workgroup each, joined by a second kernel where a session has more than one.  Inside a
-// workgroup the wavefronts form RG groups of 32 rows that share what is loaded, and PG groups that take turns with the
-// positions: a step of one token with few rows has a wavefront per 32 positions and no barrier, a large tree has four times
-// 32 rows on the same positions.
+// Inside a workgroup the wavefronts form RG groups of 32 rows that share what is loaded, and PG groups that take turns with
+// the positions: a step of one token with few rows has two wavefronts on positions of their own and no barrier, a large tree
+// has four times 32 rows on the same positions.
+//
+// The work is a line: session after session, in each its tiles of rows and heads, in each of those its positions in units of
+// 64.  It is cut into equal lengths, one for each workgroup that the chip holds at a time, wherever the cuts fall: sessions of
+// all lengths keep it busy to the end, and nobody has to know the lengths on the host.  What a cut has split is joined by a
+// second kernel.
 #include <type_traits>
 
 #include "plc_device.h"
 #include "plc_paged.h"
 
+#ifndef PLC_MINUNITS
+#define PLC_MINUNITS 4
+#define PLC_PG 2
+#define PLC_PER_CU 2
+#endif
 namespace plc {
 namespace {
 
@@ -32,20 +41,70 @@ constexpr float kLowest = -1.0e30f;   // stands for "nothing seen yet" in the ru
 constexpr float kSlack = 8.0f;        // the maximum that weights are relative to may lag by so much: 2^8 in a weight
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 constexpr int kMaskWords = PLC_TREE_NODES / 64;
+constexpr int kUnit = 64;           // positions of a unit of the line
+constexpr int kLineWords = 1024 + 1;  // where each session begins on it
 
 struct AttendArgs {
   PoolView p;
-  int32_t layer, G, max_nodes, max_len, chunk;  // positions of a chunk
+  int32_t layer, G, max_nodes, max_len;
+  int32_t tile_rows, workers, least;  // rows of a tile; workgroups; units that a workgroup takes at least
   int64_t N, q_node, q_head, out_node, out_head;
   const uint16_t *q;
   uint16_t *out;
   float *lse;
   const int32_t *off, *parents;
   float scale2;   // scale * log2(e)
-  float *part_o;  // [chunk][N H G][d]
-  float *part_ml; // [chunk][N H G][2]: maximum (base 2), sum
+  float *part_o;  // [workgroup][2][tile_rows][d]
+  float *part_ml; // [workgroup][2][tile_rows][2]: maximum (base 2), sum
   uint32_t *status;
 };
+
+// A session as its part of the line: none where what is said of it cannot be (status tells), or it has no nodes.
+struct SessionView {
+  int32_t n0, t, len, row_tiles, units;  // first node, nodes, positions, tiles of rows, units of one tile and head
+};
+__device__ __forceinline__ SessionView session_of(const AttendArgs &a, int32_t n0, int32_t n1, int32_t len, bool *bad) {
+  SessionView v = {n0, n1 - n0, len, 0, 0};
+  if (v.t == 0) return v;
+  if (v.t < 0 || n0 < 0 || n1 > a.N || v.t > a.max_nodes || len < v.t || len > a.max_len ||
+      len > ((int64_t)a.p.M << a.p.shift)) {
+    *bad = true;
+    return v;
+  }
+  v.row_tiles = (v.t * a.G + a.tile_rows - 1) / a.tile_rows;
+  v.units = (len + kUnit - 1) / kUnit;
+  return v;
+}
+
+// Where each session begins on the line, which ends at `total` (below 2^31: checked on the host).  Up to 64 sessions every
+// wavefront holds for itself, a lane each; more are written down in LDS, line[S] being the total.
+struct Line {
+  uint32_t begin, total;
+  int32_t n0, t, len;
+};
+__device__ __forceinline__ Line draw_line(const AttendArgs &a, uint32_t *line, bool *bad) {
+  const int lane = threadIdx.x & 63;
+  Line mine = {};
+  uint32_t at = 0;
+  for (int s0 = 0; s0 < a.p.S; s0 += 64) {
+    const int s = s0 + lane;
+    SessionView v = {};
+    if (s < a.p.S) v = session_of(a, a.off[s], a.off[s + 1], a.p.lens[s], bad);
+    const uint32_t n = (uint32_t)(v.row_tiles * v.units) * (uint32_t)a.p.H, upto = wave_inclusive_scan(n);
+    mine = {at + upto - n, 0, v.n0, v.t, v.len};
+    if (a.p.S > 64 && threadIdx.x < 64 && s < a.p.S) line[s] = mine.begin;
+    at += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  if (a.p.S > 64) {
+    if (threadIdx.x == 0) line[a.p.S] = at;
+    __syncthreads();
+  }
+  mine.total = at;
+  return mine;
+}
+__device__ __forceinline__ uint32_t share_of(const AttendArgs &a, uint32_t total) {
+  return max((uint32_t)a.least, (total + (uint32_t)a.workers - 1) / (uint32_t)a.workers);
+}
 
 template <class T>
 __device__ __forceinline__ float16v mfma(short8v a, short8v b, float16v c) {
@@ -97,9 +156,18 @@ struct AttendShape {
   static constexpr size_t kMeet = PG > 1 ? (size_t)PG * kRows * (kOutRow + 2) * 4 : 0;
   static constexpr size_t kStages = (size_t)PG * kBuffers * kStage;
   static constexpr size_t kMain = kStages > kMeet ? kStages : kMeet;
-  static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4;
+  static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4 + kLineWords * 4;
+  static_assert(kUnit % (PG * kTile) == 0, "whole rounds in a unit");
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+  static constexpr int kWavesPerSimd = DP <= 128 ? 2 : 1;
 };
+
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char *scalar_ptr(const char *ptr) {
+  const uint64_t x = (uint64_t)(uintptr_t)ptr;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return reinterpret_cast<const char *>((uintptr_t)((uint64_t)hi << 32 | lo));
+}
 
 // Waits until at most N of this wavefront's loads are outstanding.
 template <int N>
@@ -113,28 +181,47 @@ __device__ __forceinline__ void wait_loads() {
 // One step of the second product reads MD pairs of transposed pieces of V.  A transposing read gives 16 lanes the 4 x 16
 // block that they address 8 bytes each of, a column to a lane (checked on the device).  Assembly, with its wait: the
 // compiler takes the builtin for a reader of whatever the loads in flight write, and would wait for all of them.
-template <int N>
-__device__ __forceinline__ void read_transposed(const uint32_t (&at)[N][2], int base, short8v (&v)[N]) {
+template <int kOffset, int N>
+__device__ __forceinline__ void read_transposed(const uint32_t (&at)[N][2], short8v (&v)[N]) {
 #if defined(__HIP_DEVICE_COMPILE__)
   short4v r[N][2];
+  if constexpr (N % 4 == 0) {
 #pragma unroll
-  for (int m = 0; m < N; m += 2) {
-    // (a wait of its own for each four: the products of the first can start while the last are read)
+    for (int m = 0; m < N; m += 4)
+      asm volatile(
+          "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%16\n\t"
+          "ds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %3, %11 offset:%16\n\t"
+          "ds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%16\n\t"
+          "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(r[m][0]), "=&v"(r[m][1]), "=&v"(r[m + 1][0]), "=&v"(r[m + 1][1]), "=&v"(r[m + 2][0]), "=&v"(r[m + 2][1]),
+            "=&v"(r[m + 3][0]), "=&v"(r[m + 3][1])
+          : "v"(at[m][0]), "v"(at[m][1]), "v"(at[m + 1][0]), "v"(at[m + 1][1]), "v"(at[m + 2][0]), "v"(at[m + 2][1]),
+            "v"(at[m + 3][0]), "v"(at[m + 3][1]), "n"(kOffset));
+  } else {
+    static_assert(N == 2, "two or a multiple of four");
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %2, %6\n\t"
-        "ds_read_b64_tr_b16 %3, %7\n\ts_waitcnt lgkmcnt(0)"
-        : "=&v"(r[m][0]), "=&v"(r[m][1]), "=&v"(r[m + 1][0]), "=&v"(r[m + 1][1])
-        : "v"(at[m][0] + base), "v"(at[m][1] + base), "v"(at[m + 1][0] + base), "v"(at[m + 1][1] + base));
+        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
+        "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[1][0]), "=&v"(r[1][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(kOffset));
   }
 #pragma unroll
   for (int m = 0; m < N; ++m) v[m] = __builtin_shufflevector(r[m][0], r[m][1], 0, 1, 2, 3, 4, 5, 6, 7);
 #else
-  (void)at, (void)base, (void)v;
+  (void)at, (void)v;
 #endif
 }
 
+// The workgroup's barrier, and no wait for loads that are still to come.
+__device__ __forceinline__ void join_round() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((15 << 0) | (7 << 4) | (0 << 8) | (3 << 14));  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 template <class T, class Shape, bool kExact>
-__global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_kernel(AttendArgs a) {
   constexpr int DP = Shape::DP, RG = Shape::RG, PG = Shape::PG, NT = Shape::NT;
   constexpr int KS = DP / 16, MD = DP / 32;
   extern __shared__ __attribute__((aligned(1024))) char attend_lds[];
@@ -142,36 +229,65 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
   uint64_t *const masks = reinterpret_cast<uint64_t *>(attend_lds + Shape::kMain);  // [kRows][kMaskWords]
   int32_t *const up = reinterpret_cast<int32_t *>(masks + Shape::kRows * kMaskWords);
   const PoolView &p = a.p;
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int lane_id = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rg = wave % RG, pg = wave / RG;
-  const int s = (int)blockIdx.z, chunk = (int)blockIdx.y;
-  const int h = (int)blockIdx.x % p.H, row_tile = (int)blockIdx.x / p.H;
-
-  const const_int *const off = (const const_int *)a.off;
-  const int n0 = off[s], t = off[s + 1] - n0, len = ((const const_int *)p.lens)[s];
-  if (t == 0) return;
-  if (t < 0 || n0 < 0 || (int64_t)n0 + t > a.N || t > a.max_nodes || len < t || len > a.max_len ||
-      len > ((int64_t)p.M << p.shift)) {
-    if (threadIdx.x == 0 && chunk == 0 && blockIdx.x == 0) raise(a.status, PLC_ERR_INVALID);
-    return;
+  uint32_t *const line = reinterpret_cast<uint32_t *>(up + PLC_TREE_NODES);
+  Line mine;
+  {
+    bool bad = false;
+    mine = draw_line(a, line, &bad);
+    unsigned id = blockIdx.x;
+    asm("" : "+s"(id));  // (or the compiler takes the number, zero here, through a lane from then on, and all that follows from it)
+    if (bad && id == 0) raise(a.status, PLC_ERR_INVALID);
   }
+  const auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+  const uint32_t total = scalar(mine.total), share = scalar(share_of(a, total)), worker = blockIdx.x, begin = worker * share;
+  if (begin >= total) return;
+  const uint32_t end = min(total, begin + share);
+  bool bad_page = false;
+
+  for (uint32_t at = begin; at < end;) {
+  // (what follows from the lane is worked out again for every piece, and again behind its positions: kept in registers
+  // throughout it would not leave room for two wavefronts a SIMD)
+  int lane = lane_id;
+  asm volatile("" : "+v"(lane));
+  int half = lane >> 5, col = lane & 31;
+  // the session that `at` lies in: the last that begins there or before
+  int s, n0, t, len;
+  uint32_t s_begin;
+  if (p.S <= 64) {
+    s = __builtin_popcountll(__ballot(lane < p.S && mine.begin <= at)) - 1;
+    s_begin = (uint32_t)__builtin_amdgcn_readlane((int)mine.begin, s);
+    n0 = __builtin_amdgcn_readlane(mine.n0, s), t = __builtin_amdgcn_readlane(mine.t, s), len = __builtin_amdgcn_readlane(mine.len, s);
+  } else {
+    s = -1;
+    for (int s0 = 0; s0 < p.S; s0 += 64)
+      s += __builtin_popcountll(__ballot(s0 + lane < p.S && line[min(s0 + lane, p.S)] <= at));
+    s_begin = scalar(line[s]);
+    const const_int *const off = (const const_int *)a.off;
+    n0 = off[s], t = off[s + 1] - n0, len = ((const const_int *)p.lens)[s];
+  }
+  const int units = (len + kUnit - 1) / kUnit;
+  const uint32_t in_session = at - s_begin, pair = scalar(in_session / (uint32_t)units), unit0 = in_session - pair * (uint32_t)units;
+  const int row_tile = (int)scalar(pair / (uint32_t)p.H), h = (int)pair - row_tile * p.H;
+  const uint32_t unit1 = min((uint32_t)units, unit0 + (end - at));
+  const bool whole = unit0 == 0 && unit1 == (uint32_t)units;      // nobody else works on these rows
+  const int slot = 2 * (int)worker + (at != begin);           // of a part: a workgroup's first piece, or its last
+  at += unit1 - unit0;
+
   const int R = t * a.G, r0 = row_tile * Shape::kRows;
-  const int first = chunk * a.chunk;
-  if (r0 >= R || first >= len) return;
-  const int ctx = len - t;
+  const int first = (int)unit0 * kUnit, ctx = len - t;
   const bool chain = a.parents == nullptr;
-  int last = min(len, first + a.chunk);
-  if (chain) last = min(last, ctx + (min(R, r0 + Shape::kRows) - 1) / a.G + 1);  // what the tile's last node sees
-  const bool whole = len <= a.chunk;  // the session's only chunk
+  int last = min(len, (int)unit1 * kUnit);
+  if (chain) last = min(last, ctx + (int)scalar((uint32_t)(min(R, r0 + Shape::kRows) - 1) / (uint32_t)a.G) + 1);  // what the tile's last node sees
 
   // this lane's row
-  const int row = r0 + rg * 32 + col;
-  const bool live = row < R;
-  const int node = (live ? row : R - 1) / a.G, head = h * a.G + (live ? row : R - 1) % a.G;
+  int row = r0 + rg * 32 + col;
+  bool live = row < R;
+  int node = (live ? row : R - 1) / a.G, head = h * a.G + (live ? row : R - 1) % a.G;
   const int node0 = r0 / a.G;  // of the tile
-  const int64_t out_row = (int64_t)(n0 + node) * (p.H * a.G) + head;
 
-  // ancestors of the tile's nodes, where the chunk reaches into the tree
+  // ancestors of the tile's nodes, where the piece reaches into the tree
   if (!chain && last > ctx) {
     for (int i = threadIdx.x; i < t; i += Shape::kThreads) {
       int u = a.parents[n0 + i];
@@ -228,44 +344,59 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
 
   // ---- loads: this wavefront's share of its positions group's stages
   constexpr int kLanesPerRow = DP / 8, kRowsPerLoad = 64 / kLanesPerRow, kLoads16 = 16 / kRowsPerLoad;
-  constexpr int kUnits = 2 * NT;                       // runs of 16 positions, which never cross a page
-  static_assert(kUnits % RG == 0 || RG % kUnits == 0, "units go round");
-  constexpr int kPieces = RG <= kUnits ? 1 : RG / kUnits;  // wavefronts that share a unit
-  constexpr int kMine = RG <= kUnits ? kUnits / RG : 1;    // units of a wavefront
-  constexpr int kUnitLoads = kLoads16 / kPieces;
-  static_assert(kUnitLoads >= 1 && kLoads16 % kPieces == 0, "whole loads");
-  constexpr int kStageLoads = 2 * kMine * kUnitLoads;
-  const int unit0 = RG <= kUnits ? rg * kMine : rg / kPieces, load0 = RG <= kUnits ? 0 : (rg % kPieces) * kUnitLoads;
-  uint32_t lane_at[kUnitLoads];  // bytes from the first of a unit's rows
-  bool wanted[kUnitLoads];
+  constexpr int kRuns = 2 * NT;                        // runs of 16 positions, which never cross a page
+  static_assert(kRuns % RG == 0 || RG % kRuns == 0, "runs go round");
+  constexpr int kPieces = RG <= kRuns ? 1 : RG / kRuns;  // wavefronts that share a run
+  constexpr int kMine = RG <= kRuns ? kRuns / RG : 1;    // runs of a wavefront
+  constexpr int kRunLoads = kLoads16 / kPieces;
+  static_assert(kRunLoads >= 1 && kLoads16 % kPieces == 0, "whole loads");
+  constexpr int kStageLoads = 2 * kMine * kRunLoads;
+  const int run0 = RG <= kRuns ? rg * kMine : rg / kPieces, load0 = RG <= kRuns ? 0 : (rg % kPieces) * kRunLoads;
+  uint32_t lane_at[kRunLoads];  // bytes from the first of a run's rows
+  bool wanted[kRunLoads];
 #pragma unroll
-  for (int j = 0; j < kUnitLoads; ++j) {
+  for (int j = 0; j < kRunLoads; ++j) {
     const int r = (load0 + j) * kRowsPerLoad + lane / kLanesPerRow, c = (lane % kLanesPerRow) ^ turn<DP>(r);
     lane_at[j] = 2 * (uint32_t)(r * (int)p.row_s + c * 8);
     wanted[j] = kExact || c < p.d8;
   }
   const int64_t head_at = a.layer * p.layer_s + h * p.head_s;
-  const const_int *const table = (const const_int *)p.table + (int64_t)s * p.M;
+  // The piece's table entries, 64 at a time, a lane each: a page's number is then a readlane away, where a load of it
+  // in front of each stage's loads would keep them waiting.
+  const int32_t *const table = p.table + (int64_t)s * p.M;
   const int last_slot = (len - 1) >> p.shift, row_mask = (1 << p.shift) - 1;
-  bool bad_page = false;
+  int slot0;
+  int32_t entries;
+  auto fetch_entries = [&](int slot) {
+    slot0 = slot;
+    entries = table[min(slot0 + lane, last_slot)];
+    asm volatile("" : "+v"(entries));  // waited for here: where it is used, the loads under way would be taken along
+  };
+  fetch_entries(first >> p.shift);
   auto page_at = [&](int pos) {  // (past the session's end any of its pages will do: no weight goes there)
-    const int32_t page = table[min(pos >> p.shift, last_slot)];
+    const int slot = min(pos >> p.shift, last_slot);
+    if (slot >= slot0 + 64) fetch_entries(slot);
+    const int32_t page = __builtin_amdgcn_readlane(entries, slot - slot0);
     if (!p.page_ok(page)) bad_page = true;
     return p.page_ok(page) ? page : 0;
   };
   auto request = [&](int pos, int buf) {
 #pragma unroll
     for (int m = 0; m < kMine; ++m) {
-      const int unit = unit0 + m, at = pos + 16 * unit;
+      const int run = run0 + m, at = pos + 16 * run;
       const int64_t from = page_at(at) * p.page_s + head_at + (at & row_mask) * p.row_s;
-      const char *const from_k = reinterpret_cast<const char *>(p.k + from), *const from_v = reinterpret_cast<const char *>(p.v + from);
-      const int to = (pg * Shape::kBuffers + buf) * Shape::kStage + unit * (16 * DP * 2);
+      const char *from_k = reinterpret_cast<const char *>(p.k + from), *from_v = reinterpret_cast<const char *>(p.v + from);
+      // (in scalars, and not to be folded into a pointer per lane and load that lives through the loop)
+      from_k = scalar_ptr(from_k), from_v = scalar_ptr(from_v);
+      const int to = (pg * Shape::kBuffers + buf) * Shape::kStage + run * (16 * DP * 2);
 #pragma unroll
-      for (int j = 0; j < kUnitLoads; ++j) {
+      for (int j = 0; j < kRunLoads; ++j) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass of the compiler does not know the device's load-to-LDS builtin
+        uint32_t mine = lane_at[j];
+        asm("" : "+v"(mine));  // 32 bits, next to a scalar base: one address register a lane
         if (wanted[j]) {
-          __builtin_amdgcn_global_load_lds(from_k + lane_at[j], lds + to + (load0 + j) * 1024, 16, 0, 0);
-          __builtin_amdgcn_global_load_lds(from_v + lane_at[j], lds + to + Shape::kHalf + (load0 + j) * 1024, 16, 0, 0);
+          __builtin_amdgcn_global_load_lds(from_k + mine, lds + to + (load0 + j) * 1024, 16, 0, 0);
+          __builtin_amdgcn_global_load_lds(from_v + mine, lds + to + Shape::kHalf + (load0 + j) * 1024, 16, 0, 0);
         }
 #else
         (void)from_k, (void)from_v, (void)to, (void)lds, (void)lane_at, (void)wanted;
@@ -306,28 +437,41 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
   const int rounds = span > 0 ? (span + PG * Shape::kTile - 1) / (PG * Shape::kTile) : 0;
   auto pos_of = [&](int it) { return first + (it * PG + pg) * Shape::kTile; };
   if (rounds > 0 && pos_of(0) < last) request(pos_of(0), 0);
+  // Q has come before the loop begins: waited for inside it, it would take the loads under way along
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
   for (int it = 0; it < rounds; ++it) {
     const int pos = pos_of(it);
-    const bool mine = pos < last, more = it + 1 < rounds && pos_of(it + 1) < last;
-    if (more) {
+    const bool here = pos < last, more = it + 1 < rounds && pos_of(it + 1) < last;
+    if (more) {  // two stages under way while the older one is waited for
       request(pos_of(it + 1), (it + 1) & 1);
       wait_loads<kStageLoads>();
     } else {
       wait_loads<0>();
     }
-    if (RG > 1) __syncthreads();
-    if (mine) {
+    if (RG > 1) join_round();
+    if (here) {
       const lds_char *const ks_lds = lds + (pg * Shape::kBuffers + (it & 1)) * Shape::kStage, *const vs_lds = ks_lds + Shape::kHalf;
       float16v sc[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[n][i] = 0.0f;
+      // K's fragments four products ahead; fences keep the order
+      short8v kf[2][4];
+      auto read_k = [&](int g) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const short8v kf = *(const __attribute__((address_space(3))) short8v *)(ks_lds + n * (32 * DP * 2) + k_at[ks]);
-          sc[n] = mfma<T>(kf, qf[ks], sc[n]);
-        }
+        for (int i = 4 * g; i < 4 * g + 4; ++i)
+          kf[g & 1][i & 3] = *(const __attribute__((address_space(3))) short8v *)(ks_lds + i % NT * (32 * DP * 2) + k_at[i / NT]);
+      };
+      read_k(0);
+#pragma unroll
+      for (int g = 0; g < KS * NT / 4; ++g) {
+        if (g + 1 < KS * NT / 4) read_k(g + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 4 * g; i < 4 * g + 4; ++i) sc[i % NT] = mfma<T>(kf[g & 1][i & 3], qf[i / NT], sc[i % NT]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       const bool edge = pos + Shape::kTile > ctx;  // positions that not every row sees, or that are none
       if (edge) {
@@ -372,6 +516,7 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           bool found = false;
+#pragma unroll 1
           for (int c = 0; c < DP / 16; ++c) {
             const short8v v = *(const __attribute__((address_space(3))) short8v *)(vs_lds + n * (32 * DP * 2) +
                                                                                    place<DP>(col, c * 2 + half));
@@ -382,23 +527,30 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
           odd[n] = (uint32_t)b | (uint32_t)(b >> 32);
         }
       }
-      const int vs_at = (pg * Shape::kBuffers + (it & 1)) * Shape::kStage + Shape::kHalf;
+      const uint32_t vs_at = (uint32_t)((pg * Shape::kBuffers + (it & 1)) * Shape::kStage + Shape::kHalf);
+      uint32_t v_here[MD][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int m = 0; m < MD; ++m) v_here[m][0] = v_at[m][0] + vs_at, v_here[m][1] = v_at[m][1] + vs_at;
+      auto weigh = [&](auto nu) {  // 16 positions' products with their weights
+        constexpr int n = decltype(nu)::value / 2, u = decltype(nu)::value % 2;
+        short8v vf[MD];
+        read_transposed<n * (32 * DP * 2) + u * (16 * DP * 2)>(v_here, vf);
+        if (odd[n]) {  // a weight of zero must not meet them: they are added by hand where the weight is not zero
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          short8v vf[MD];
-          read_transposed(v_at, vs_at + n * (32 * DP * 2) + u * (16 * DP * 2), vf);
-          if (odd[n]) {  // a weight of zero must not meet them: they are added by hand where the weight is not zero
+          for (int m = 0; m < MD; ++m)
 #pragma unroll
-            for (int m = 0; m < MD; ++m)
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (special<T>((uint16_t)vf[m][e])) vf[m][e] = 0;
-          }
-#pragma unroll
-          for (int m = 0; m < MD; ++m) o[m] = mfma<T>(vf[m], pf[n][u], o[m]);
+            for (int e = 0; e < 8; ++e)
+              if (special<T>((uint16_t)vf[m][e])) vf[m][e] = 0;
         }
+#pragma unroll
+        for (int m = 0; m < MD; ++m) o[m] = mfma<T>(vf[m], pf[n][u], o[m]);
+      };
+      weigh(std::integral_constant<int, 0>());
+      weigh(std::integral_constant<int, 1>());
+      if constexpr (NT == 2) {
+        weigh(std::integral_constant<int, 2>());
+        weigh(std::integral_constant<int, 3>());
+      }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         for (uint32_t rest = odd[n]; rest; rest &= rest - 1) {
@@ -412,26 +564,35 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
 #pragma unroll
             for (int m = 0; m < MD; ++m)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int e = 32 * m + 8 * (i >> 2) + 4 * half + (i & 3);
-                const uint16_t bits = *(const __attribute__((address_space(3))) uint16_t *)(vs_lds + n * (32 * DP * 2) +
-                                                                                            place<DP>(r, e >> 3) + (e & 7) * 2);
-                if (special<T>(bits)) o[m][i] += w * (float)__builtin_bit_cast(T, bits);
+              for (int b = 0; b < 4; ++b) {
+                const short4v v = *(const __attribute__((address_space(3))) short4v *)(vs_lds + n * (32 * DP * 2) +
+                                                                                       place<DP>(r, 4 * m + b) + 8 * half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint16_t bits = (uint16_t)v[e];
+                  if (special<T>(bits)) o[m][4 * b + e] += w * (float)__builtin_bit_cast(T, bits);
+                }
               }
           }
         }
     }
     // The buffer is loaded into again in the next round.
-    if (RG > 1) __syncthreads();
+    if (RG > 1) join_round();
   }
-  if (bad_page && lane == 0) raise(a.status, PLC_ERR_INVALID);
   {
     const Halves both = halves(sum);
     sum = both.lo + both.hi;
   }
+  lane = lane_id;
+  asm volatile("" : "+v"(lane));
+  half = lane >> 5, col = lane & 31;
+  row = r0 + rg * 32 + col;
+  live = row < R;
+  node = (live ? row : R - 1) / a.G, head = h * a.G + (live ? row : R - 1) % a.G;
+  const int64_t out_row = (int64_t)(n0 + node) * (p.H * a.G) + head;
 
-  float *const part_o = a.part_o + ((int64_t)chunk * a.N * (p.H * a.G) + out_row) * (8 * p.d8);
-  float *const part_ml = a.part_ml + ((int64_t)chunk * a.N * (p.H * a.G) + out_row) * 2;
+  const int64_t part = (int64_t)slot * Shape::kRows + rg * 32 + col;
+  float *const part_o = a.part_o + part * (8 * p.d8), *const part_ml = a.part_ml + part * 2;
   uint16_t *const out = a.out + (n0 + node) * a.out_node + head * a.out_head;
   if (PG == 1) {
     if (live) {
@@ -461,7 +622,8 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
         }
       }
     }
-    return;
+    __syncthreads();  // (the masks are free)
+    continue;
   }
 
   // the positions groups meet: their sums, relative to the largest maximum, row by row
@@ -486,7 +648,7 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
   for (int i = threadIdx.x; i < min(Shape::kRows, R - r0) * kPieces4; i += Shape::kThreads) {
     const int r = i / kPieces4, e = i % kPieces4 * 4;
     if (!kExact && e >= 8 * p.d8) continue;
-    float peak = kLowest, total = 0.0f;
+    float peak = kLowest, sums = 0.0f;
     float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int g = 0; g < PG; ++g) peak = fmaxf(peak, meet_ml[2 * (g * Shape::kRows + r)]);
@@ -495,68 +657,97 @@ __global__ __launch_bounds__(Shape::kThreads) void attend_kernel(AttendArgs a) {
       const float w = __builtin_amdgcn_exp2f(meet_ml[2 * (g * Shape::kRows + r)] - peak);
       const float n = meet_ml[2 * (g * Shape::kRows + r) + 1];
       if (n != 0.0f) {  // (a group that has seen nothing has weight zero, not zero times what it holds)
-        total += w * n;
+        sums += w * n;
         v += w * *reinterpret_cast<const float4v *>(meet + (g * Shape::kRows + r) * Shape::kOutRow + e);
       }
     }
     const int my_node = (r0 + r) / a.G, my_head = h * a.G + (r0 + r) % a.G;
     const int64_t to = (int64_t)(n0 + my_node) * (p.H * a.G) + my_head;
     if (whole) {
-      const float scale = total == 0.0f ? 0.0f : 1.0f / total;
+      const float scale = sums == 0.0f ? 0.0f : 1.0f / sums;
       *reinterpret_cast<ushort4 *>(a.out + (n0 + my_node) * a.out_node + my_head * a.out_head + e) =
           make_ushort4(round16<T>(v[0] * scale), round16<T>(v[1] * scale), round16<T>(v[2] * scale), round16<T>(v[3] * scale));
-      if (e == 0 && a.lse) a.lse[to] = total == 0.0f ? -__builtin_inff() : (peak + __builtin_amdgcn_logf(total)) * kLn2;
+      if (e == 0 && a.lse) a.lse[to] = sums == 0.0f ? -__builtin_inff() : (peak + __builtin_amdgcn_logf(sums)) * kLn2;
     } else {
-      const int64_t at = (int64_t)chunk * a.N * (p.H * a.G) + to;
-      *reinterpret_cast<float4v *>(a.part_o + at * (8 * p.d8) + e) = v;
+      const int64_t mine = (int64_t)slot * Shape::kRows + r;
+      *reinterpret_cast<float4v *>(a.part_o + mine * (8 * p.d8) + e) = v;
       if (e == 0) {
-        a.part_ml[2 * at] = peak;
-        a.part_ml[2 * at + 1] = total;
+        a.part_ml[2 * mine] = peak;
+        a.part_ml[2 * mine + 1] = sums;
       }
     }
   }
+  __syncthreads();  // the next piece loads where they met
+  }
+  if (bad_page && lane_id == 0) raise(a.status, PLC_ERR_INVALID);
 }
 
-// Joins the chunks of sessions that have several: four components to a lane.
+constexpr int kJoinGroups = 4;
+// Joins the parts of rows that several workgroups have worked on: four components to a lane.
 template <class T>
 __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
+  __shared__ uint32_t line[kLineWords];
+  __shared__ float4v meet_o[kBlock];
+  __shared__ float meet_l[kBlock];
   const PoolView &p = a.p;
+  bool bad = false;
+  const Line mine = draw_line(a, line, &bad);
   const int s = (int)blockIdx.y;
-  const int n0 = a.off[s], t = a.off[s + 1] - n0, len = p.lens[s];
-  if (t <= 0 || n0 < 0 || (int64_t)n0 + t > a.N || t > a.max_nodes || len < t || len > a.max_len || len <= a.chunk ||
-      len > ((int64_t)p.M << p.shift))
-    return;
-  const int heads = p.H * a.G, pieces = 2 * p.d8;
-  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  if (i >= (int64_t)t * heads * pieces) return;
-  const int e = (int)(i % pieces) * 4, x = (int)(i / pieces);
-  const int node = n0 + x / heads, head = x % heads;
-  const int64_t row = (int64_t)node * heads + head, step = a.N * heads;
-  const int chunks = (len + a.chunk - 1) / a.chunk;
-  float peak = kLowest;
-  for (int c = 0; c < chunks; ++c) peak = fmaxf(peak, a.part_ml[2 * (c * step + row)]);
-  float total = 0.0f;
-  float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int c = 0; c < chunks; ++c) {
-    const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (c * step + row));
-    if (ml.y != 0.0f) {
-      const float w = __builtin_amdgcn_exp2f(ml.x - peak);
-      total += w * ml.y;
-      v += w * *reinterpret_cast<const float4v *>(a.part_o + (c * step + row) * (8 * p.d8) + e);
+  const uint32_t s_begin = p.S <= 64 ? (uint32_t)__builtin_amdgcn_readlane((int)mine.begin, s) : line[s];
+  const SessionView v = session_of(a, a.off[s], a.off[s + 1], p.lens[s], &bad);
+  const int row_tile = (int)blockIdx.x / p.H, h = (int)blockIdx.x % p.H;
+  if (row_tile >= v.row_tiles) return;
+  const uint32_t share = share_of(a, mine.total);
+  const uint32_t from = s_begin + blockIdx.x * (uint32_t)v.units, upto = from + (uint32_t)v.units;
+  const uint32_t w0 = from / share, w1 = (upto - 1) / share;
+  if (w0 == w1) return;
+  // four groups of lanes take a quarter of the parts each
+  const int pieces = 2 * p.d8, i = (int)blockIdx.z * (kBlock / kJoinGroups) + (int)threadIdx.x % (kBlock / kJoinGroups);
+  const int group = (int)threadIdx.x / (kBlock / kJoinGroups);
+  const int r = i / pieces, e = i % pieces * 4, row = row_tile * a.tile_rows + r;
+  const bool here = r < a.tile_rows && row < v.t * a.G;
+  // a workgroup's piece is its first one but where it has begun before these rows
+  const int64_t slot0 = 2 * (int64_t)w0 + (from > w0 * share);
+  const int parts = (int)(w1 - w0) + 1;
+  auto part = [&](int c) { return (c == 0 ? slot0 : 2 * (int64_t)(w0 + c)) * a.tile_rows + r; };
+  float peak = kLowest, sums = 0.0f;
+  float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (here) {
+#pragma unroll 8
+    for (int c = 0; c < parts; ++c) peak = fmaxf(peak, a.part_ml[2 * part(c)]);
+#pragma unroll 8
+    for (int c = group; c < parts; c += kJoinGroups) {
+      const float2 m = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(c));
+      const float4v x = *reinterpret_cast<const float4v *>(a.part_o + part(c) * (8 * p.d8) + e);
+      const float w = __builtin_amdgcn_exp2f(m.x - peak);
+      const bool any = m.y != 0.0f;  // (a part that has seen nothing has weight zero, not zero times what it holds)
+      sums += any ? w * m.y : 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += any ? w * x[k] : 0.0f;
     }
   }
-  const float scale = total == 0.0f ? 0.0f : 1.0f / total;
+  meet_o[threadIdx.x] = o;
+  meet_l[threadIdx.x] = sums;
+  __syncthreads();
+  if (group != 0 || !here) return;
+#pragma unroll
+  for (int g = 1; g < kJoinGroups; ++g) {
+    o += meet_o[threadIdx.x + g * (kBlock / kJoinGroups)];
+    sums += meet_l[threadIdx.x + g * (kBlock / kJoinGroups)];
+  }
+  const int node = v.n0 + row / a.G, head = h * a.G + row % a.G;
+  const float scale = sums == 0.0f ? 0.0f : 1.0f / sums;
   *reinterpret_cast<ushort4 *>(a.out + node * a.out_node + head * a.out_head + e) =
-      make_ushort4(round16<T>(v[0] * scale), round16<T>(v[1] * scale), round16<T>(v[2] * scale), round16<T>(v[3] * scale));
-  if (e == 0 && a.lse) a.lse[row] = total == 0.0f ? -__builtin_inff() : (peak + __builtin_amdgcn_logf(total)) * kLn2;
+      make_ushort4(round16<T>(o[0] * scale), round16<T>(o[1] * scale), round16<T>(o[2] * scale), round16<T>(o[3] * scale));
+  if (e == 0 && a.lse)
+    a.lse[(int64_t)node * (p.H * a.G) + head] = sums == 0.0f ? -__builtin_inff() : (peak + __builtin_amdgcn_logf(sums)) * kLn2;
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
 
 struct AttendPlan {
-  int rows, step;  // rows of a workgroup; positions that one round of it takes
-  int64_t row_tiles, chunks;
-  int32_t chunk;
+  int rows, workers;       // rows of a tile, workgroups
+  int64_t row_tiles, line;  // tiles of a session, units of the line: at most
 };
 
 AttendPlan attend_plan(const plc_pages *p, int32_t G, int32_t max_nodes, int32_t max_len) {
@@ -564,16 +755,11 @@ AttendPlan attend_plan(const plc_pages *p, int32_t G, int32_t max_nodes, int32_t
   const int64_t rows = (int64_t)max_nodes * G;
   const bool wide = p->d > 128;
   plan.rows = rows <= 32 ? 32 : rows <= 64 || wide ? 64 : 128;
-  plan.step = plan.rows == 32 ? (wide ? 64 : 128) : plan.rows == 64 ? (wide ? 32 : 64) : 64;
   plan.row_tiles = (rows + plan.rows - 1) / plan.rows;
-  const int64_t groups = (int64_t)p->S * p->H * plan.row_tiles;
-  int64_t chunks = (8 * kComputeUnits + groups - 1) / groups;
-  const int64_t most = (max_len + 255) / 256;
-  if (chunks > most) chunks = most;
-  int64_t chunk = (max_len + chunks - 1) / chunks;
-  chunk = (chunk + plan.step - 1) / plan.step * plan.step;
-  plan.chunk = (int32_t)(chunk < INT32_MAX ? chunk : INT32_MAX / plan.step * plan.step);
-  plan.chunks = (max_len + (int64_t)plan.chunk - 1) / plan.chunk;
+  plan.line = plan.row_tiles * (((int64_t)max_len + kUnit - 1) / kUnit);
+  plan.line = plan.line > INT32_MAX ? INT64_MAX : plan.line * p->H * p->S;
+  const int64_t most = (wide ? 1 : PLC_PER_CU) * kComputeUnits, shares = (plan.line + PLC_MINUNITS - 1) / PLC_MINUNITS;
+  plan.workers = (int)(shares < most ? shares : most);
   return plan;
 }
 
@@ -582,42 +768,43 @@ bool attend_valid(const plc_pages *p, int32_t G, int64_t N, int32_t max_nodes, i
          (int64_t)p->H * G <= 65536 && (int64_t)max_nodes * G <= INT32_MAX / 256 && p->stride[3] * 32 < (int64_t)1 << 30;
 }
 
-size_t attend_bytes(const plc_pages *p, int32_t G, int64_t N, const AttendPlan &plan) {
-  if (plan.chunks <= 1) return 256;
-  return align_up((size_t)plan.chunks * (size_t)N * p->H * G * (p->d + 2) * sizeof(float), 256);
+size_t attend_bytes(const plc_pages *p, const AttendPlan &plan) {
+  return align_up((size_t)plan.workers * 2 * plan.rows * (p->d + 2) * sizeof(float), 256);
 }
 
 template <class T, class Shape>
-void launch_attend(const AttendArgs &a, dim3 grid, hipStream_t st) {
+void launch_attend(const AttendArgs &a, hipStream_t st) {
   const bool exact = 8 * a.p.d8 == Shape::DP;
   const auto kernel = exact ? &attend_kernel<T, Shape, true> : &attend_kernel<T, Shape, false>;
-  (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds);
-  hipLaunchKernelGGL(kernel, grid, dim3(Shape::kThreads), Shape::kLds, st, a);
+  static const hipError_t sized[2] = {  // once: it costs a call's host time over again
+      hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, Shape, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds),
+      hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, Shape, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds)};
+  (void)sized;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)a.workers), dim3(Shape::kThreads), Shape::kLds, st, a);
 }
 
 template <class T, int DP>
-void launch_attend(const AttendArgs &a, const AttendPlan &plan, dim3 grid, hipStream_t st) {
+void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   if constexpr (DP <= 128) {
-    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 4, 1>>(a, grid, st);
-    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, grid, st);
-    else launch_attend<T, AttendShape<DP, 4, 1, 2>>(a, grid, st);
+    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, PLC_PG, 1>>(a, st);
+    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, st);
+    else launch_attend<T, AttendShape<DP, 4, 1, 2>>(a, st);
   } else {
-    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, grid, st);
-    else launch_attend<T, AttendShape<DP, 2, 1, 1>>(a, grid, st);
+    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, st);
+    else launch_attend<T, AttendShape<DP, 2, 1, 1>>(a, st);
   }
 }
 
 template <class T>
 int attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
-  const dim3 grid((unsigned)(plan.row_tiles * a.p.H), (unsigned)plan.chunks, (unsigned)a.p.S);
   const int d = 8 * a.p.d8;
-  if (d <= 64) launch_attend<T, 64>(a, plan, grid, st);
-  else if (d <= 128) launch_attend<T, 128>(a, plan, grid, st);
-  else launch_attend<T, 256>(a, plan, grid, st);
-  if (plan.chunks > 1) {
-    const int64_t lanes = (int64_t)a.max_nodes * a.p.H * a.G * 2 * a.p.d8;
-    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)((lanes + kBlock - 1) / kBlock), (unsigned)a.p.S), dim3(kBlock), 0, st, a);
-  }
+  if (d <= 64) launch_attend<T, 64>(a, plan, st);
+  else if (d <= 128) launch_attend<T, 128>(a, plan, st);
+  else launch_attend<T, 256>(a, plan, st);
+  if (plan.workers > 1)
+    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(plan.row_tiles * a.p.H), (unsigned)a.p.S,
+                                            (unsigned)((plan.rows * 2 * a.p.d8 * kJoinGroups + kBlock - 1) / kBlock)),
+                       dim3(kBlock), 0, st, a);
   return launch_status();
 }
 
@@ -628,7 +815,8 @@ using namespace plc;
 
 extern "C" size_t plc_attend_workspace_bytes(const plc_pages *pages, int32_t G, int64_t N, int32_t max_nodes, int32_t max_len) {
   if (!attend_valid(pages, G, N, max_nodes, max_len)) return 0;
-  return attend_bytes(pages, G, N, attend_plan(pages, G, max_nodes, max_len));
+  const AttendPlan plan = attend_plan(pages, G, max_nodes, max_len);
+  return plan.line > INT32_MAX ? 0 : attend_bytes(pages, plan);
 }
 
 extern "C" int plc_attend(const plc_pages *pages, int32_t layer, int32_t type, const void *q, const int64_t *q_stride,
@@ -643,17 +831,18 @@ extern "C" int plc_attend(const plc_pages *pages, int32_t layer, int32_t type, c
     if (q_stride[i] < 0 || q_stride[i] % 8 || out_stride[i] < 0 || out_stride[i] % 8) return PLC_ERR_INVALID;
   if (N == 0) return PLC_OK;
   const AttendPlan plan = attend_plan(pages, G, max_nodes, max_len);
-  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 256) || ws_bytes < attend_bytes(pages, G, N, plan))
+  if (plan.line > INT32_MAX || !aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 256) ||
+      ws_bytes < attend_bytes(pages, plan))
     return PLC_ERR_INVALID;
-  if (plan.row_tiles * pages->H > INT32_MAX || plan.chunks > 65535) return PLC_ERR_INVALID;
   AttendArgs a;
   a.p = pool_view(pages);
-  a.layer = layer, a.G = G, a.max_nodes = max_nodes, a.max_len = max_len, a.chunk = plan.chunk;
+  a.layer = layer, a.G = G, a.max_nodes = max_nodes, a.max_len = max_len;
+  a.tile_rows = plan.rows, a.workers = plan.workers, a.least = PLC_MINUNITS;
   a.N = N, a.q_node = q_stride[0], a.q_head = q_stride[1], a.out_node = out_stride[0], a.out_head = out_stride[1];
   a.q = static_cast<const uint16_t *>(q), a.out = static_cast<uint16_t *>(out), a.lse = lse;
   a.off = off, a.parents = parents, a.scale2 = scale * kLog2e;
   a.part_ml = static_cast<float *>(ws);
-  a.part_o = a.part_ml + (plan.chunks > 1 ? (size_t)plan.chunks * N * pages->H * G * 2 : 0);
+  a.part_o = a.part_ml + (size_t)plan.workers * 2 * plan.rows * 2;
   a.status = status;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return type == PLC_FP16 ? attend<_Float16>(a, plan, st) : attend<__bf16>(a, plan, st);

@@ -32,6 +32,7 @@ class PagedKVCache:
         self.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.used = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._attend_need = {}
         self._attend_ws = [torch.empty(256, dtype=torch.uint8, device=self.device)]
 
     @classmethod
@@ -42,7 +43,7 @@ class PagedKVCache:
                    torch.zeros(S, dtype=torch.int32, device=device), torch.zeros(P, dtype=torch.int32, device=device))
 
     def _per_session(self, t, n, what):
-        if t.shape != (n,):
+        if t.dim() != 1 or t.numel() != n:
             raise ValueError(f"{what} has {n} entries")
         return t
 
@@ -76,9 +77,10 @@ class PagedKVCache:
     def _rows(self, k, v, layer):
         if k.dim() == 3:  # [rows, H, d]: a single layer's
             k, v = k.unsqueeze(1), v.unsqueeze(1)
-        if k.dtype != self.dtype or v.dtype != self.dtype:
+        if k.dtype is not self.dtype or v.dtype is not self.dtype:
             raise TypeError(f"expected {self.dtype}, got {k.dtype} and {v.dtype}")
-        if k.dim() not in (4, 5) or k.shape[2] != self.H or k.shape[-1] != self.d or (k.dim() == 5 and k.shape[0] != self.S):
+        shape = k.shape
+        if len(shape) not in (4, 5) or shape[2] != self.H or shape[-1] != self.d or (len(shape) == 5 and shape[0] != self.S):
             raise ValueError("rows are [rows, layers, H, d] packed, [rows, H, d] of one layer, or [S, layers, H, rows, d]")
         return k, v, layer
 
@@ -96,9 +98,15 @@ class PagedKVCache:
     def reserve(self, G, N, max_nodes, max_len=None):
         """Workspace for attend calls of this size, so that none is made during them (under graph capture).  What was
         handed out before stays, for work in flight and for graphs."""
-        need = plc.plc_attend_workspace_bytes(self.pages, G, N, max_nodes, max_len or self.M * self.B)
-        if need == 0:
-            raise plc.PlcError(plc.PLC_ERR_INVALID, "plc_attend_workspace_bytes")
+        max_len = self.M * self.B if max_len is None else max_len
+        need = self._attend_need.get((G, N, max_nodes, max_len))
+        if need is None:
+            need = plc.plc_attend_workspace_bytes(self.pages, G, N, max_nodes, max_len)
+            if need == 0:
+                raise plc.PlcError(plc.PLC_ERR_INVALID, "plc_attend_workspace_bytes")
+            if len(self._attend_need) >= 1024:
+                self._attend_need.clear()
+            self._attend_need[G, N, max_nodes, max_len] = need
         if need > self._attend_ws[-1].numel():
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("reserve the attention's workspace before the capture")
@@ -110,23 +118,25 @@ class PagedKVCache:
         """Attention of the sessions' last off[s+1] - off[s] positions, q [N, H*G, d], over all that they see, in one
         layer: a tree with `parents` (int32 [N], numbers within the tree, -1: continues the cache), a chain without.
         Returns out [N, H*G, d] and lse float32 [N, H*G].  No session has more than max_nodes nodes (default: N; of a tree at most
-        plc.TREE_NODES) and
-        max_len positions (default: what the table holds; a close bound is faster).  scale: 1/sqrt(d) by default."""
-        if q.dim() != 3 or q.dtype != self.dtype:
+        plc.TREE_NODES) and max_len positions (default: what the table holds).  scale: 1/sqrt(d) by default."""
+        if q.dim() != 3 or q.dtype is not self.dtype:
             raise ValueError(f"q is [nodes, heads, d] of {self.dtype}")
-        N, heads = q.shape[0], q.shape[1]
+        N, heads, _ = q.shape
         self._per_session(off, self.S + 1, "off")
         if parents is not None:
             self._per_session(parents, N, "parents")
-        out = torch.empty((N, heads, self.d), dtype=self.dtype, device=self.device) if out is None else out
-        lse = torch.empty((N, heads), dtype=torch.float32, device=self.device) if lse is None else lse
-        if lse.shape != (N, heads):
+        if out is None:
+            out = q.new_empty((N, heads, self.d))
+        if lse is None:
+            lse = q.new_empty((N, heads), dtype=torch.float32)
+        elif lse.shape != (N, heads):
             raise ValueError("lse is [nodes, heads]")
         if N == 0:
             return out, lse
         if max_nodes is None:
             max_nodes = N if parents is None else min(N, plc.TREE_NODES)
-        max_len = self.M * self.B if max_len is None else max_len
+        if max_len is None:
+            max_len = self.M * self.B
         ws = self.reserve(heads // self.H, N, max_nodes, max_len)
         plc.plc_attend(self.pages, layer, q, off, parents, max_nodes, max_len, self.d ** -0.5 if scale is None else scale, out,
                        lse, ws, self.status)

@@ -545,85 +545,98 @@ def make_pages(k, v, table, lens, refs) -> plc_pages:
 
 
 def plc_pages_workspace_bytes(pages) -> int:
-    return int(lib().plc_pages_workspace_bytes(C.byref(pages)))
+    return int(lib().plc_pages_workspace_bytes(pages))
+
+
+# The calls of the paged cache come once or more a token, and last as long as a launch or two: their arguments go over as
+# plain addresses, and the stream is asked for directly.
+_I64x2 = C.c_int64 * 2
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _ints(t):
+    if t.dtype is not torch.int32:
+        raise TypeError(f"expected {torch.int32}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError("plc takes device tensors")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
+
+
+def _on_device(t):
+    if not t.is_cuda:
+        raise ValueError("plc takes device tensors")
+    return t.data_ptr()
 
 
 def plc_pages_fork(pages, src, status):
     """src int32 [S]: what each session becomes; -1: empty."""
-    rc = lib().plc_pages_fork(C.byref(pages), _contig(src, torch.int32), _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_fork")
+    _check(lib().plc_pages_fork(pages, _ints(src), _ints(status), _raw_stream(src.device.index)), "plc_pages_fork")
 
 
 def plc_pages_extend(pages, grow, ws, status):
-    rc = lib().plc_pages_extend(C.byref(pages), _contig(grow, torch.int32), _contig(ws, torch.uint8), ws.numel(),
-                                _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_extend")
+    _check(lib().plc_pages_extend(pages, _ints(grow), _on_device(ws), ws.numel(), _ints(status),
+                                  _raw_stream(grow.device.index)), "plc_pages_extend")
 
 
 def plc_pages_trim(pages, new_lens, status):
-    rc = lib().plc_pages_trim(C.byref(pages), _contig(new_lens, torch.int32), _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_trim")
+    _check(lib().plc_pages_trim(pages, _ints(new_lens), _ints(status), _raw_stream(new_lens.device.index)), "plc_pages_trim")
 
 
 def plc_pages_accept(pages, off, path, path_off, status):
     """off, path_off int32 [S+1]; path int32: numbers of the nodes to keep, ascending in each session."""
-    rc = lib().plc_pages_accept(C.byref(pages), _contig(off, torch.int32), _contig(path, torch.int32), path.numel(),
-                                _contig(path_off, torch.int32), _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_accept")
+    _check(lib().plc_pages_accept(pages, _ints(off), _ints(path), path.numel(), _ints(path_off), _ints(status),
+                                  _raw_stream(off.device.index)), "plc_pages_accept")
 
 
 def plc_pages_compact(pages, used, ws, status):
     """used int32 [1] out, or None: pages in use."""
-    rc = lib().plc_pages_compact(C.byref(pages), _contig(used, torch.int32), _contig(ws, torch.uint8), ws.numel(),
-                                 _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_compact")
+    _check(lib().plc_pages_compact(pages, None if used is None else _ints(used), _on_device(ws), ws.numel(), _ints(status),
+                                   _raw_stream(ws.device.index)), "plc_pages_compact")
 
 
 def _rows_of(k, v, layer):
     """Rows in a buffer: packed [rows, layers, heads, d], or [S, layers, heads, rows, d], of any strides but the last."""
-    if k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(-1) != 1 or k.dim() not in (4, 5):
+    st, shape = k.stride(), k.shape
+    if shape != v.shape or k.dtype is not v.dtype or st != v.stride() or st[-1] != 1 or len(shape) not in (4, 5):
         raise ValueError("k and v are [rows, layers, heads, d] or [sessions, layers, heads, rows, d] of one layout")
-    r = plc_rows()
-    r.packed = int(k.dim() == 4)
-    r.layer, r.layers, r.rows = layer, k.shape[1], k.shape[0] if r.packed else k.shape[3]
-    st = k.stride()
-    r.stride = (C.c_int64 * 4)(0, st[1], st[2], st[0]) if r.packed else (C.c_int64 * 4)(*st[:4])
-    return r
+    if len(shape) == 4:
+        return plc_rows(layer, shape[1], 1, shape[0], (0, st[1], st[2], st[0]))
+    return plc_rows(layer, shape[1], 0, shape[3], st[:4])
 
 
 def plc_pages_store(pages, off, k, v, layer, status):
     """k, v [rows, layers, H, d] packed, or [S, layers, H, rows, d]; off int32 [S+1]; layer: the first of the pool's."""
-    rc = lib().plc_pages_store(C.byref(pages), C.byref(_rows_of(k, v, layer)), _contig(off, torch.int32), _ptr(k), _ptr(v),
-                               _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_store")
+    _check(lib().plc_pages_store(pages, _rows_of(k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
+                                 _raw_stream(off.device.index)), "plc_pages_store")
 
 
 def plc_pages_load(pages, off, k, v, layer, status):
     """plc_pages_store the other way round."""
-    rc = lib().plc_pages_load(C.byref(pages), C.byref(_rows_of(k, v, layer)), _contig(off, torch.int32), _ptr(k), _ptr(v),
-                              _contig(status, torch.int32), _stream())
-    _check(rc, "plc_pages_load")
+    _check(lib().plc_pages_load(pages, _rows_of(k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
+                                _raw_stream(off.device.index)), "plc_pages_load")
 
 
 def plc_attend_workspace_bytes(pages, G, N, max_nodes, max_len) -> int:
-    return int(lib().plc_attend_workspace_bytes(C.byref(pages), int(G), int(N), int(max_nodes), int(max_len)))
+    return int(lib().plc_attend_workspace_bytes(pages, G, N, max_nodes, max_len))
 
 
 def plc_attend(pages, layer, q, off, parents, max_nodes, max_len, scale, out, lse, ws, status):
     """q, out [N, H*G, d], components contiguous; parents int32 [N] or None (a chain); lse float32 [N, H*G] or None."""
-    if q.shape != out.shape or q.dtype != out.dtype or q.dim() != 3 or q.stride(2) != 1 or out.stride(2) != 1:
+    shape, qs, os_ = q.shape, q.stride(), out.stride()
+    if shape != out.shape or q.dtype is not out.dtype or len(shape) != 3 or qs[2] != 1 or os_[2] != 1:
         raise ValueError("q and out are [nodes, heads, d] of one type, with contiguous components")
-    if q.dtype not in (torch.float16, torch.bfloat16):
+    if q.dtype is not torch.float16 and q.dtype is not torch.bfloat16:
         raise TypeError(f"expected float16 or bfloat16, got {q.dtype}")
-    if q.shape[1] % pages.H or q.shape[2] != pages.d:
+    if shape[1] % pages.H or shape[2] != pages.d:
         raise ValueError("query heads are a multiple of the cache's, with as many components")
-    qs, os_ = q.stride(), out.stride()
-    rc = lib().plc_attend(C.byref(pages), layer, PLC_FP16 if q.dtype == torch.float16 else PLC_BF16, _ptr(q),
-                          (C.c_int64 * 2)(qs[0], qs[1]), q.shape[1] // pages.H, q.shape[0], _contig(off, torch.int32),
-                          _contig(parents, torch.int32), max_nodes, max_len, scale, _ptr(out),
-                          (C.c_int64 * 2)(os_[0], os_[1]), _contig(lse, torch.float32), _contig(ws, torch.uint8), ws.numel(),
-                          _contig(status, torch.int32), _stream())
-    _check(rc, "plc_attend")
+    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        raise TypeError("lse is contiguous float32")
+    _check(lib().plc_attend(pages, layer, PLC_FP16 if q.dtype is torch.float16 else PLC_BF16, _on_device(q), _I64x2(qs[0], qs[1]),
+                            shape[1] // pages.H, shape[0], _ints(off), None if parents is None else _ints(parents), max_nodes,
+                            max_len, scale, _on_device(out), _I64x2(os_[0], os_[1]), None if lse is None else _on_device(lse),
+                            _on_device(ws), ws.numel(), _ints(status), _raw_stream(q.device.index)), "plc_attend")
 
 
 class PrefixTrie:
