@@ -636,7 +636,7 @@ typedef struct plc_pages {
                              contiguous                                                                  */
   int32_t P, L, H, B, d;  /* pages, layers, KV heads, rows of a page (a power of two, 16..1024), components
                              (a multiple of 8)                                                           */
-  int32_t S, M;           /* sessions (1..1024), entries of a session                                    */
+  int32_t S, M;           /* sessions (1..1024), entries of a session (M * B <= 2^30)                    */
   int32_t *table, *lens, *refs;
 } plc_pages;
 
@@ -706,8 +706,8 @@ int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *
  *   parents    nullable: i32 [N], the number within the tree of a node's parent, less than its own; -1: the node
  *              continues the cache.
  *   max_nodes, max_len   host: no session has more nodes, none more positions (else status PLC_ERR_INVALID is
- *              raised and the session's rows are left alone).  They set the launch: max_len close to the longest
- *              session's length is best.  With `parents` max_nodes <= PLC_TREE_NODES.
+ *              raised and the session's rows are left alone).  They set the launch: close bounds are best.  With
+ *              `parents` max_nodes <= PLC_TREE_NODES.
  *   lse        out, nullable: fp32 [N, H*G].
  *   ws         plc_attend_workspace_bytes(), 256-byte aligned.
  */

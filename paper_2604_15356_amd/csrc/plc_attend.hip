@@ -12,20 +12,14 @@
 // the positions: a step of one token with few rows has two wavefronts on positions of their own and no barrier, a large tree
 // has four times 32 rows on the same positions.
 //
-// The work is a line: session after session, in each its tiles of rows and heads, in each of those its positions in units of
-// 64.  It is cut into equal lengths, one for each workgroup that the chip holds at a time, wherever the cuts fall: sessions of
-// all lengths keep it busy to the end, and nobody has to know the lengths on the host.  What a cut has split is joined by a
-// second kernel.
+// The work is a line of chunks: session after session, in each its tiles of rows and heads, in each of those its positions,
+// cut where they are long, or where there are few rows and heads to fill the chip with (attend_plan has the rule).
+// Workgroups take the chunks in turn; what a cut has split is joined by a second kernel.
 #include <type_traits>
 
 #include "plc_device.h"
 #include "plc_paged.h"
 
-#ifndef PLC_MINUNITS
-#define PLC_MINUNITS 4
-#define PLC_PG 2
-#define PLC_PER_CU 2
-#endif
 namespace plc {
 namespace {
 
@@ -41,27 +35,26 @@ constexpr float kLowest = -1.0e30f;   // stands for "nothing seen yet" in the ru
 constexpr float kSlack = 8.0f;        // the maximum that weights are relative to may lag by so much: 2^8 in a weight
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 constexpr int kMaskWords = PLC_TREE_NODES / 64;
-constexpr int kUnit = 64;           // positions of a unit of the line
 constexpr int kLineWords = 1024 + 1;  // where each session begins on it
 
 struct AttendArgs {
   PoolView p;
   int32_t layer, G, max_nodes, max_len;
-  int32_t tile_rows, workers, least;  // rows of a tile; workgroups; units that a workgroup takes at least
+  int32_t tile_rows, chunk;  // rows of a tile, positions of a chunk
   int64_t N, q_node, q_head, out_node, out_head;
   const uint16_t *q;
   uint16_t *out;
   float *lse;
   const int32_t *off, *parents;
   float scale2;   // scale * log2(e)
-  float *part_o;  // [workgroup][2][tile_rows][d]
-  float *part_ml; // [workgroup][2][tile_rows][2]: maximum (base 2), sum
+  float *part_o;  // [chunk][tile_rows][d]
+  float *part_ml; // [chunk][tile_rows][2]: maximum (base 2), sum
   uint32_t *status;
 };
 
 // A session as its part of the line: none where what is said of it cannot be (status tells), or it has no nodes.
 struct SessionView {
-  int32_t n0, t, len, row_tiles, units;  // first node, nodes, positions, tiles of rows, units of one tile and head
+  int32_t n0, t, len, row_tiles, chunks;  // first node, nodes, positions, tiles of rows, chunks of one tile and head
 };
 __device__ __forceinline__ SessionView session_of(const AttendArgs &a, int32_t n0, int32_t n1, int32_t len, bool *bad) {
   SessionView v = {n0, n1 - n0, len, 0, 0};
@@ -72,7 +65,7 @@ __device__ __forceinline__ SessionView session_of(const AttendArgs &a, int32_t n
     return v;
   }
   v.row_tiles = (v.t * a.G + a.tile_rows - 1) / a.tile_rows;
-  v.units = (len + kUnit - 1) / kUnit;
+  v.chunks = (int32_t)(((uint32_t)len + (uint32_t)a.chunk - 1) / (uint32_t)a.chunk);
   return v;
 }
 
@@ -90,7 +83,7 @@ __device__ __forceinline__ Line draw_line(const AttendArgs &a, uint32_t *line, b
     const int s = s0 + lane;
     SessionView v = {};
     if (s < a.p.S) v = session_of(a, a.off[s], a.off[s + 1], a.p.lens[s], bad);
-    const uint32_t n = (uint32_t)(v.row_tiles * v.units) * (uint32_t)a.p.H, upto = wave_inclusive_scan(n);
+    const uint32_t n = (uint32_t)(v.row_tiles * v.chunks) * (uint32_t)a.p.H, upto = wave_inclusive_scan(n);
     mine = {at + upto - n, 0, v.n0, v.t, v.len};
     if (a.p.S > 64 && threadIdx.x < 64 && s < a.p.S) line[s] = mine.begin;
     at += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
@@ -101,9 +94,6 @@ __device__ __forceinline__ Line draw_line(const AttendArgs &a, uint32_t *line, b
   }
   mine.total = at;
   return mine;
-}
-__device__ __forceinline__ uint32_t share_of(const AttendArgs &a, uint32_t total) {
-  return max((uint32_t)a.least, (total + (uint32_t)a.workers - 1) / (uint32_t)a.workers);
 }
 
 template <class T>
@@ -157,7 +147,7 @@ struct AttendShape {
   static constexpr size_t kStages = (size_t)PG * kBuffers * kStage;
   static constexpr size_t kMain = kStages > kMeet ? kStages : kMeet;
   static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4 + kLineWords * 4;
-  static_assert(kUnit % (PG * kTile) == 0, "whole rounds in a unit");
+  
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   static constexpr int kWavesPerSimd = DP <= 128 ? 2 : 1;
 };
@@ -241,13 +231,11 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     if (bad && id == 0) raise(a.status, PLC_ERR_INVALID);
   }
   const auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-  const uint32_t total = scalar(mine.total), share = scalar(share_of(a, total)), worker = blockIdx.x, begin = worker * share;
-  if (begin >= total) return;
-  const uint32_t end = min(total, begin + share);
+  const uint32_t total = scalar(mine.total);
   bool bad_page = false;
 
-  for (uint32_t at = begin; at < end;) {
-  // (what follows from the lane is worked out again for every piece, and again behind its positions: kept in registers
+  for (uint32_t at = blockIdx.x; at < total; at += gridDim.x) {
+  // (what follows from the lane is worked out again for every chunk, and again behind its positions: kept in registers
   // throughout it would not leave room for two wavefronts a SIMD)
   int lane = lane_id;
   asm volatile("" : "+v"(lane));
@@ -267,18 +255,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     const const_int *const off = (const const_int *)a.off;
     n0 = off[s], t = off[s + 1] - n0, len = ((const const_int *)p.lens)[s];
   }
-  const int units = (len + kUnit - 1) / kUnit;
-  const uint32_t in_session = at - s_begin, pair = scalar(in_session / (uint32_t)units), unit0 = in_session - pair * (uint32_t)units;
+  const uint32_t chunks = scalar(((uint32_t)len + (uint32_t)a.chunk - 1) / (uint32_t)a.chunk);
+  const uint32_t pair = scalar((at - s_begin) / chunks), nth = at - s_begin - pair * chunks;
   const int row_tile = (int)scalar(pair / (uint32_t)p.H), h = (int)pair - row_tile * p.H;
-  const uint32_t unit1 = min((uint32_t)units, unit0 + (end - at));
-  const bool whole = unit0 == 0 && unit1 == (uint32_t)units;      // nobody else works on these rows
-  const int slot = 2 * (int)worker + (at != begin);           // of a part: a workgroup's first piece, or its last
-  at += unit1 - unit0;
+  const bool whole = chunks == 1;
 
   const int R = t * a.G, r0 = row_tile * Shape::kRows;
-  const int first = (int)unit0 * kUnit, ctx = len - t;
+  const int first = (int)nth * a.chunk, ctx = len - t;
   const bool chain = a.parents == nullptr;
-  int last = min(len, (int)unit1 * kUnit);
+  int last = min(len - first, a.chunk) + first;
   if (chain) last = min(last, ctx + (int)scalar((uint32_t)(min(R, r0 + Shape::kRows) - 1) / (uint32_t)a.G) + 1);  // what the tile's last node sees
 
   // this lane's row
@@ -287,7 +272,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   int node = (live ? row : R - 1) / a.G, head = h * a.G + (live ? row : R - 1) % a.G;
   const int node0 = r0 / a.G;  // of the tile
 
-  // ancestors of the tile's nodes, where the piece reaches into the tree
+  // ancestors of the tile's nodes, where the chunk reaches into the tree
   if (!chain && last > ctx) {
     for (int i = threadIdx.x; i < t; i += Shape::kThreads) {
       int u = a.parents[n0 + i];
@@ -361,7 +346,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     wanted[j] = kExact || c < p.d8;
   }
   const int64_t head_at = a.layer * p.layer_s + h * p.head_s;
-  // The piece's table entries, 64 at a time, a lane each: a page's number is then a readlane away, where a load of it
+  // The chunk's table entries, 64 at a time, a lane each: a page's number is then a readlane away, where a load of it
   // in front of each stage's loads would keep them waiting.
   const int32_t *const table = p.table + (int64_t)s * p.M;
   const int last_slot = (len - 1) >> p.shift, row_mask = (1 << p.shift) - 1;
@@ -591,7 +576,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   node = (live ? row : R - 1) / a.G, head = h * a.G + (live ? row : R - 1) % a.G;
   const int64_t out_row = (int64_t)(n0 + node) * (p.H * a.G) + head;
 
-  const int64_t part = (int64_t)slot * Shape::kRows + rg * 32 + col;
+  const int64_t part = (int64_t)at * Shape::kRows + rg * 32 + col;
   float *const part_o = a.part_o + part * (8 * p.d8), *const part_ml = a.part_ml + part * 2;
   uint16_t *const out = a.out + (n0 + node) * a.out_node + head * a.out_head;
   if (PG == 1) {
@@ -669,7 +654,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
           make_ushort4(round16<T>(v[0] * scale), round16<T>(v[1] * scale), round16<T>(v[2] * scale), round16<T>(v[3] * scale));
       if (e == 0 && a.lse) a.lse[to] = sums == 0.0f ? -__builtin_inff() : (peak + __builtin_amdgcn_logf(sums)) * kLn2;
     } else {
-      const int64_t mine = (int64_t)slot * Shape::kRows + r;
+      const int64_t mine = (int64_t)at * Shape::kRows + r;
       *reinterpret_cast<float4v *>(a.part_o + mine * (8 * p.d8) + e) = v;
       if (e == 0) {
         a.part_ml[2 * mine] = peak;
@@ -677,13 +662,13 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       }
     }
   }
-  __syncthreads();  // the next piece loads where they met
+  __syncthreads();  // the next chunk loads where they met
   }
   if (bad_page && lane_id == 0) raise(a.status, PLC_ERR_INVALID);
 }
 
 constexpr int kJoinGroups = 4;
-// Joins the parts of rows that several workgroups have worked on: four components to a lane.
+// Joins the chunks of rows whose positions were cut: four components to a lane.
 template <class T>
 __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   __shared__ uint32_t line[kLineWords];
@@ -697,19 +682,15 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   const SessionView v = session_of(a, a.off[s], a.off[s + 1], p.lens[s], &bad);
   const int row_tile = (int)blockIdx.x / p.H, h = (int)blockIdx.x % p.H;
   if (row_tile >= v.row_tiles) return;
-  const uint32_t share = share_of(a, mine.total);
-  const uint32_t from = s_begin + blockIdx.x * (uint32_t)v.units, upto = from + (uint32_t)v.units;
-  const uint32_t w0 = from / share, w1 = (upto - 1) / share;
-  if (w0 == w1) return;
+  const int parts = v.chunks;
+  if (parts <= 1) return;
+  const int64_t part0 = (int64_t)s_begin + (int64_t)blockIdx.x * parts;
   // four groups of lanes take a quarter of the parts each
   const int pieces = 2 * p.d8, i = (int)blockIdx.z * (kBlock / kJoinGroups) + (int)threadIdx.x % (kBlock / kJoinGroups);
   const int group = (int)threadIdx.x / (kBlock / kJoinGroups);
   const int r = i / pieces, e = i % pieces * 4, row = row_tile * a.tile_rows + r;
   const bool here = r < a.tile_rows && row < v.t * a.G;
-  // a workgroup's piece is its first one but where it has begun before these rows
-  const int64_t slot0 = 2 * (int64_t)w0 + (from > w0 * share);
-  const int parts = (int)(w1 - w0) + 1;
-  auto part = [&](int c) { return (c == 0 ? slot0 : 2 * (int64_t)(w0 + c)) * a.tile_rows + r; };
+  auto part = [&](int c) { return (part0 + c) * a.tile_rows + r; };
   float peak = kLowest, sums = 0.0f;
   float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
   if (here) {
@@ -746,9 +727,14 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
 // ---- host side ------------------------------------------------------------------------------------------------------------
 
 struct AttendPlan {
-  int rows, workers;       // rows of a tile, workgroups
-  int64_t row_tiles, line;  // tiles of a session, units of the line: at most
+  int rows;                        // of a tile
+  int32_t chunk;                   // positions
+  int64_t row_tiles, parts, line;  // tiles of a session, chunks of a tile and head, chunks of all: at most
 };
+
+constexpr int64_t kMostGroups = 2048;  // workgroups: bounds from the host may be far above what there is to do
+constexpr int kLongest = 8192;         // positions of a chunk
+constexpr int64_t kPartRows = 131072;  // rows of partial results, at most, that long contexts of many sessions are cut for
 
 AttendPlan attend_plan(const plc_pages *p, int32_t G, int32_t max_nodes, int32_t max_len) {
   AttendPlan plan;
@@ -756,10 +742,25 @@ AttendPlan attend_plan(const plc_pages *p, int32_t G, int32_t max_nodes, int32_t
   const bool wide = p->d > 128;
   plan.rows = rows <= 32 ? 32 : rows <= 64 || wide ? 64 : 128;
   plan.row_tiles = (rows + plan.rows - 1) / plan.rows;
-  plan.line = plan.row_tiles * (((int64_t)max_len + kUnit - 1) / kUnit);
-  plan.line = plan.line > INT32_MAX ? INT64_MAX : plan.line * p->H * p->S;
-  const int64_t most = (wide ? 1 : PLC_PER_CU) * kComputeUnits, shares = (plan.line + PLC_MINUNITS - 1) / PLC_MINUNITS;
-  plan.workers = (int)(shares < most ? shares : most);
+  const int64_t pairs = plan.row_tiles * p->H * p->S;
+  // A chunk is a workgroup's work.  Whole positions of a tile of rows and head need no joining (a launch, 5 us), and where
+  // there is one for every compute unit nothing is gained by cutting them: 64 sessions x 8 heads of up to 4000 positions
+  // 108 us, cut in two 121 us.  Fewer are cut until there are as many chunks as the chip holds workgroups, one a compute
+  // unit for a single tile of 32 rows, two for more: one session of 16,000 positions 20 us, in twice as many chunks 28 us.
+  // Short ones are quicker done by one workgroup (500 positions 7.7 against 10.1 us, 1000 positions 10.8 against 9.8).
+  int64_t chunk = max_len;
+  const bool small = plan.rows == 32;
+  if (max_len > (small ? 768 : 384)) {
+    const int64_t target = small ? kComputeUnits : 2 * kComputeUnits;
+    if (pairs < kComputeUnits) chunk = (max_len * pairs + target - 1) / target;
+    chunk = chunk > kLongest ? kLongest : chunk;
+    const int64_t most = kPartRows / plan.rows / pairs;  // parts
+    if (most < 2) chunk = max_len;
+    else if (chunk * most < max_len) chunk = (max_len + most - 1) / most;
+  }
+  plan.chunk = (int32_t)(chunk > INT32_MAX - 128 ? INT32_MAX - 127 : (chunk + 127) / 128 * 128);
+  plan.parts = (max_len + (int64_t)plan.chunk - 1) / plan.chunk;
+  plan.line = pairs > INT32_MAX ? INT64_MAX : pairs * plan.parts;
   return plan;
 }
 
@@ -769,29 +770,30 @@ bool attend_valid(const plc_pages *p, int32_t G, int64_t N, int32_t max_nodes, i
 }
 
 size_t attend_bytes(const plc_pages *p, const AttendPlan &plan) {
-  return align_up((size_t)plan.workers * 2 * plan.rows * (p->d + 2) * sizeof(float), 256);
+  if (plan.parts <= 1) return 256;
+  return align_up((size_t)plan.line * plan.rows * (p->d + 2) * sizeof(float), 256);
 }
 
 template <class T, class Shape>
-void launch_attend(const AttendArgs &a, hipStream_t st) {
+void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   const bool exact = 8 * a.p.d8 == Shape::DP;
   const auto kernel = exact ? &attend_kernel<T, Shape, true> : &attend_kernel<T, Shape, false>;
   static const hipError_t sized[2] = {  // once: it costs a call's host time over again
       hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, Shape, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds),
       hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, Shape, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds)};
   (void)sized;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)a.workers), dim3(Shape::kThreads), Shape::kLds, st, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.line < kMostGroups ? plan.line : kMostGroups)), dim3(Shape::kThreads), Shape::kLds, st, a);
 }
 
 template <class T, int DP>
 void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   if constexpr (DP <= 128) {
-    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, PLC_PG, 1>>(a, st);
-    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, st);
-    else launch_attend<T, AttendShape<DP, 4, 1, 2>>(a, st);
+    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 4, 1>>(a, plan, st);
+    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, plan, st);
+    else launch_attend<T, AttendShape<DP, 4, 1, 2>>(a, plan, st);
   } else {
-    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, st);
-    else launch_attend<T, AttendShape<DP, 2, 1, 1>>(a, st);
+    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, plan, st);
+    else launch_attend<T, AttendShape<DP, 2, 1, 1>>(a, plan, st);
   }
 }
 
@@ -801,9 +803,10 @@ int attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   if (d <= 64) launch_attend<T, 64>(a, plan, st);
   else if (d <= 128) launch_attend<T, 128>(a, plan, st);
   else launch_attend<T, 256>(a, plan, st);
-  if (plan.workers > 1)
+  const int64_t joined = (int64_t)a.max_nodes * a.G < plan.rows ? (int64_t)a.max_nodes * a.G : plan.rows;  // rows of a tile
+  if (plan.parts > 1)
     hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(plan.row_tiles * a.p.H), (unsigned)a.p.S,
-                                            (unsigned)((plan.rows * 2 * a.p.d8 * kJoinGroups + kBlock - 1) / kBlock)),
+                                            (unsigned)((joined * 2 * a.p.d8 * kJoinGroups + kBlock - 1) / kBlock)),
                        dim3(kBlock), 0, st, a);
   return launch_status();
 }
@@ -837,12 +840,12 @@ extern "C" int plc_attend(const plc_pages *pages, int32_t layer, int32_t type, c
   AttendArgs a;
   a.p = pool_view(pages);
   a.layer = layer, a.G = G, a.max_nodes = max_nodes, a.max_len = max_len;
-  a.tile_rows = plan.rows, a.workers = plan.workers, a.least = PLC_MINUNITS;
+  a.tile_rows = plan.rows, a.chunk = plan.chunk;
   a.N = N, a.q_node = q_stride[0], a.q_head = q_stride[1], a.out_node = out_stride[0], a.out_head = out_stride[1];
   a.q = static_cast<const uint16_t *>(q), a.out = static_cast<uint16_t *>(out), a.lse = lse;
   a.off = off, a.parents = parents, a.scale2 = scale * kLog2e;
   a.part_ml = static_cast<float *>(ws);
-  a.part_o = a.part_ml + (size_t)plan.workers * 2 * plan.rows * 2;
+  a.part_o = a.part_ml + (plan.parts > 1 ? (size_t)plan.line * plan.rows * 2 : 0);
   a.status = status;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return type == PLC_FP16 ? attend<_Float16>(a, plan, st) : attend<__bf16>(a, plan, st);

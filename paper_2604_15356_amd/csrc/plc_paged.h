@@ -21,7 +21,7 @@ inline bool pages_valid(const plc_pages *p) {
   if (!p || !aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->table, 4) || !aligned(p->lens, 4) || !aligned(p->refs, 4))
     return false;
   if (p->P < 1 || p->L < 1 || p->H < 1 || p->S < 1 || p->S > 1024 || p->M < 1 || p->d < 8 || p->d % 8) return false;
-  if (p->B < 16 || p->B > 1024 || (p->B & (p->B - 1)) || (int64_t)p->M * p->B > INT32_MAX) return false;
+  if (p->B < 16 || p->B > 1024 || (p->B & (p->B - 1)) || (int64_t)p->M * p->B > (int64_t)1 << 30) return false;
   if ((int64_t)p->L * p->H > INT32_MAX / (2 * (int64_t)p->d)) return false;
   for (int i = 0; i < 4; ++i)
     if (p->stride[i] < 0 || p->stride[i] % 8) return false;

@@ -107,12 +107,15 @@ def test_arguments_that_are_refused():
     assert attend(N=0) == plc.PLC_OK
     assert L.plc_attend(C.byref(_pages(d=264, stride3=264)), 0, 0, P, st, 2, 5, P, None, 5, 64, 1.0, P, st, P, P, BIG, P,
                         None) == bad
-    # the workspace: two parts of a tile of rows for each workgroup, however long the sessions
-    small, large = plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 64), plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 1 << 20)
-    assert small % 256 == 0 and large % 256 == 0 and 2 * 32 * 66 * 4 <= small < large <= 1 << 26
-    assert large == plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 1 << 24)
-    assert plc.plc_attend_workspace_bytes(_pages(S=1024), 2, 1 << 20, 1 << 20, 1 << 20) == 0  # more than 32 bits count
-    assert attend(pages=C.byref(_pages(S=1024)), N=1 << 20, nodes=1 << 20, len=1 << 20) == bad
+    # the workspace: partial results of every chunk where positions are cut, and that not without end
+    assert plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 64) == 256
+    assert plc.plc_attend_workspace_bytes(_pages(), 2, 5, 5, 1 << 20) >= 2 * 2 * 3 * 32 * 66 * 4
+    for S in (1, 3, 64, 1024):
+        for nodes in (1, 40, 256, 5000):
+            n = plc.plc_attend_workspace_bytes(_pages(S=S), 2, S * nodes, nodes, 1 << 24)
+            assert n % 256 == 0 and 256 <= n <= 2 * 131072 * 66 * 4
+    assert plc.plc_attend_workspace_bytes(_pages(S=1024, H=1024), 2, 1 << 20, 1 << 20, 64) == 0  # tiles beyond 32 bits
+    assert attend(pages=C.byref(_pages(S=1024, H=1024)), N=1 << 20, nodes=1 << 20, G=2) == bad
 
 
 def test_tensors_that_the_binding_refuses():
