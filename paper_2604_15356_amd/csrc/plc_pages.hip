@@ -273,7 +273,21 @@ __global__ __launch_bounds__(kManager) void compact_kernel(PoolView p, MoveList 
 
 // ---- rows ---------------------------------------------------------------------------------------------------------------
 
+// 16 bytes of a row.  Past the caches (kStream) where more is stored than they hold: 1.07 GB in and out 195 us, through them
+// 208 us, 134 MB 24.9 against 28.8 us; but 67 MB, there from the call before, 14.2 against 12.3 us.  Rows that are loaded gain
+// nothing by it (537 MB 114 against 110 us), and the encoder reads them next.
+template <bool kStream>
+__device__ __forceinline__ uint4 get16(const uint16_t *p) {
+  return kStream ? load16_stream(p) : *reinterpret_cast<const uint4 *>(p);
+}
+template <bool kStream>
+__device__ __forceinline__ void put16(uint16_t *p, uint4 v) {
+  if (kStream) store16_stream(p, v);
+  else *reinterpret_cast<uint4 *>(p) = v;
+}
+
 // The first `rows` rows of a page's heads slab, slab + step, ... (of both halves) from one page to another.
+template <bool kStream>
 __device__ __forceinline__ void copy_slabs(const PoolView &p, int64_t from, int64_t to, int32_t rows, int32_t slab0,
                                            int32_t slab1) {
   const int32_t items = rows * p.d8;
@@ -286,16 +300,16 @@ __device__ __forceinline__ void copy_slabs(const PoolView &p, int64_t from, int6
       for (int u = 0; u < 4; ++u) {
         const int32_t lh = min(slab + u, slab1 - 1);
         const int64_t at = from * p.page_s + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + in_slab;
-        k[u] = *reinterpret_cast<const uint4 *>(p.k + at);
-        v[u] = *reinterpret_cast<const uint4 *>(p.v + at);
+        k[u] = get16<kStream>(p.k + at);
+        v[u] = get16<kStream>(p.v + at);
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int32_t lh = slab + u;
         if (lh < slab1) {
           const int64_t at = to * p.page_s + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + in_slab;
-          *reinterpret_cast<uint4 *>(p.k + at) = k[u];
-          *reinterpret_cast<uint4 *>(p.v + at) = v[u];
+          put16<kStream>(p.k + at, k[u]);
+          put16<kStream>(p.v + at, v[u]);
         }
       }
     }
@@ -308,7 +322,7 @@ __global__ __launch_bounds__(kBlock) void copy_tails_kernel(PoolView p, const Co
   const uint32_t i = blockIdx.y;
   if (i >= copies->count) return;
   const int32_t slab = (int32_t)blockIdx.x * kSlabs, slabs = p.L * p.H;
-  copy_slabs(p, copies->from[i], copies->to[i], copies->rows[i], slab, min(slab + kSlabs, slabs));
+  copy_slabs<false>(p, copies->from[i], copies->to[i], copies->rows[i], slab, min(slab + kSlabs, slabs));
 }
 
 // The first `table_blocks` workgroups rewrite the tables, the others copy pages.
@@ -335,7 +349,7 @@ __global__ __launch_bounds__(kBlock) void move_pages_kernel(PoolView p, const Mo
   const int64_t units = (int64_t)count * per_page;
   for (int64_t u = (int32_t)blockIdx.x - table_blocks; u < units; u += (int32_t)gridDim.x - table_blocks) {
     const int32_t i = (int32_t)(u / per_page), slab = (int32_t)(u % per_page) * kSlabs;
-    copy_slabs(p, movers[i], holes[i], 1 << p.shift, slab, min(slab + kSlabs, slabs));
+    copy_slabs<true>(p, movers[i], holes[i], 1 << p.shift, slab, min(slab + kSlabs, slabs));
   }
 }
 
@@ -385,10 +399,10 @@ __global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const i
         uint4 row[kPathBatch];
 #pragma unroll
         for (int u = 0; u < kPathBatch; ++u)
-          if (from[b + u] >= 0) row[u] = *reinterpret_cast<const uint4 *>(base + from[b + u]);
+          if (from[b + u] >= 0) row[u] = get16<false>(base + from[b + u]);
 #pragma unroll
         for (int u = 0; u < kPathBatch; ++u)
-          if (from[b + u] >= 0) *reinterpret_cast<uint4 *>(base + to[b + u]) = row[u];
+          if (from[b + u] >= 0) put16<false>(base + to[b + u], row[u]);
       }
     }
   }
@@ -396,13 +410,13 @@ __global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const i
 
 // Rows between a caller's buffer and pages.  A workgroup takes a block of consecutive rows, as many as give each thread 16
 // bytes of one head, works out where they are, and goes through a run of heads.
-constexpr int kHeadRun = 8;
+constexpr int kHeadRun = 4;
 struct RowsView {
   uint16_t *k, *v;
   int64_t rows, sess_s, layer_s, head_s, row_s;
   int32_t layer, layers, packed, per_block;
 };
-template <bool kStore>
+template <bool kStore, bool kStream>
 __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, const int32_t *__restrict__ off,
                                                       uint32_t *status) {
   extern __shared__ int64_t rows_lds[];  // [per_block] in the pool, [per_block] in the buffer, then off i32 [S + 1]
@@ -467,15 +481,15 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, co
       for (int u = 0; u < 4; ++u) {
         const int32_t e = min(lh + u, lh1 - 1), l = e / p.H, h = e - l * p.H;
         const int64_t at_pool = pool + l * p.layer_s + h * p.head_s, at_buf = buf + l * r.layer_s + h * r.head_s;
-        k[u] = *reinterpret_cast<const uint4 *>((kStore ? r.k : p.k) + (kStore ? at_buf : at_pool));
-        v[u] = *reinterpret_cast<const uint4 *>((kStore ? r.v : p.v) + (kStore ? at_buf : at_pool));
+        k[u] = get16<kStream>((kStore ? r.k : p.k) + (kStore ? at_buf : at_pool));
+        v[u] = get16<kStream>((kStore ? r.v : p.v) + (kStore ? at_buf : at_pool));
         to[u] = kStore ? at_pool : at_buf;
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         if (lh + u < lh1) {
-          *reinterpret_cast<uint4 *>((kStore ? p.k : r.k) + to[u]) = k[u];
-          *reinterpret_cast<uint4 *>((kStore ? p.v : r.v) + to[u]) = v[u];
+          put16<kStream>((kStore ? p.k : r.k) + to[u], k[u]);
+          put16<kStream>((kStore ? p.v : r.v) + to[u], v[u]);
         }
       }
     }
@@ -483,6 +497,8 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, co
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kCached = (int64_t)96 << 20;  // bytes moved, in and out
 
 size_t copy_list_bytes() { return align_up(sizeof(CopyList), 256); }
 size_t workspace_bytes(const plc_pages *pages) {
@@ -512,8 +528,9 @@ int move_rows(bool store, const plc_pages *pages, const plc_rows *rows, const in
   if (bx > INT32_MAX || by > 65535) return PLC_ERR_INVALID;
   const size_t lds = 16 * (size_t)r.per_block + 4 * (size_t)(p.S + 1);
   const dim3 grid((unsigned)bx, (unsigned)by);
-  if (store) hipLaunchKernelGGL(rows_kernel<true>, grid, dim3(kBlock), lds, st, p, r, off, status);
-  else hipLaunchKernelGGL(rows_kernel<false>, grid, dim3(kBlock), lds, st, p, r, off, status);
+  const bool stream = total * r.layers * p.H * p.d8 * 64 > kCached;  // of both halves, in and out
+  const auto kernel = !store ? &rows_kernel<false, false> : stream ? &rows_kernel<true, true> : &rows_kernel<true, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, st, p, r, off, status);
   return launch_status();
 }
 
