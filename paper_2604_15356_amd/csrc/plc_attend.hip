@@ -168,35 +168,47 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
-// One step of the second product reads MD pairs of transposed pieces of V.  A transposing read gives 16 lanes the 4 x 16
-// block that they address 8 bytes each of, a column to a lane (checked on the device).  Assembly, with its wait: the
-// compiler takes the builtin for a reader of whatever the loads in flight write, and would wait for all of them.
-template <int kOffset, int N>
-__device__ __forceinline__ void read_transposed(const uint32_t (&at)[N][2], short8v (&v)[N]) {
+// A step of the second product takes 16 positions, of which it reads N pairs of transposed pieces of V; two steps' reads go
+// out together (kApart: bytes between them).  A transposing read gives 16 lanes the 4 x 16 block that they address 8 bytes
+// each of, a column to a lane (checked on the device).  Assembly, with its wait: the compiler takes the builtin for a reader
+// of whatever the loads in flight write, and would wait for all of them.
+template <int kOffset, int kApart, int N>
+__device__ __forceinline__ void read_transposed(const uint32_t (&at)[N][2], short8v (&v)[2][N]) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  short4v r[N][2];
-  if constexpr (N % 4 == 0) {
+  short4v r[2][N][2];
+  if constexpr (N == 2) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %2, %10 offset:%12\n\tds_read_b64_tr_b16 %3, %11 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%13\n\tds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %6, %10 offset:%13\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0][0][0]), "=&v"(r[0][0][1]), "=&v"(r[0][1][0]), "=&v"(r[0][1][1]), "=&v"(r[1][0][0]), "=&v"(r[1][0][1]),
+          "=&v"(r[1][1][0]), "=&v"(r[1][1][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(kOffset), "n"(kOffset + kApart));
+  } else {
+    static_assert(N % 4 == 0, "two or a multiple of four");
 #pragma unroll
     for (int m = 0; m < N; m += 4)
       asm volatile(
-          "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%16\n\t"
-          "ds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %3, %11 offset:%16\n\t"
-          "ds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%16\n\t"
-          "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%16\n\ts_waitcnt lgkmcnt(0)"
-          : "=&v"(r[m][0]), "=&v"(r[m][1]), "=&v"(r[m + 1][0]), "=&v"(r[m + 1][1]), "=&v"(r[m + 2][0]), "=&v"(r[m + 2][1]),
-            "=&v"(r[m + 3][0]), "=&v"(r[m + 3][1])
+          "ds_read_b64_tr_b16 %0, %16 offset:%24\n\tds_read_b64_tr_b16 %1, %17 offset:%24\n\t"
+          "ds_read_b64_tr_b16 %2, %18 offset:%24\n\tds_read_b64_tr_b16 %3, %19 offset:%24\n\t"
+          "ds_read_b64_tr_b16 %4, %20 offset:%24\n\tds_read_b64_tr_b16 %5, %21 offset:%24\n\t"
+          "ds_read_b64_tr_b16 %6, %22 offset:%24\n\tds_read_b64_tr_b16 %7, %23 offset:%24\n\t"
+          "ds_read_b64_tr_b16 %8, %16 offset:%25\n\tds_read_b64_tr_b16 %9, %17 offset:%25\n\t"
+          "ds_read_b64_tr_b16 %10, %18 offset:%25\n\tds_read_b64_tr_b16 %11, %19 offset:%25\n\t"
+          "ds_read_b64_tr_b16 %12, %20 offset:%25\n\tds_read_b64_tr_b16 %13, %21 offset:%25\n\t"
+          "ds_read_b64_tr_b16 %14, %22 offset:%25\n\tds_read_b64_tr_b16 %15, %23 offset:%25\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(r[0][m][0]), "=&v"(r[0][m][1]), "=&v"(r[0][m + 1][0]), "=&v"(r[0][m + 1][1]), "=&v"(r[0][m + 2][0]),
+            "=&v"(r[0][m + 2][1]), "=&v"(r[0][m + 3][0]), "=&v"(r[0][m + 3][1]), "=&v"(r[1][m][0]), "=&v"(r[1][m][1]),
+            "=&v"(r[1][m + 1][0]), "=&v"(r[1][m + 1][1]), "=&v"(r[1][m + 2][0]), "=&v"(r[1][m + 2][1]), "=&v"(r[1][m + 3][0]),
+            "=&v"(r[1][m + 3][1])
           : "v"(at[m][0]), "v"(at[m][1]), "v"(at[m + 1][0]), "v"(at[m + 1][1]), "v"(at[m + 2][0]), "v"(at[m + 2][1]),
-            "v"(at[m + 3][0]), "v"(at[m + 3][1]), "n"(kOffset));
-  } else {
-    static_assert(N == 2, "two or a multiple of four");
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
-        "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
-        : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[1][0]), "=&v"(r[1][1])
-        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(kOffset));
+            "v"(at[m + 3][0]), "v"(at[m + 3][1]), "n"(kOffset), "n"(kOffset + kApart));
   }
 #pragma unroll
-  for (int m = 0; m < N; ++m) v[m] = __builtin_shufflevector(r[m][0], r[m][1], 0, 1, 2, 3, 4, 5, 6, 7);
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int m = 0; m < N; ++m) v[u][m] = __builtin_shufflevector(r[u][m][0], r[u][m][1], 0, 1, 2, 3, 4, 5, 6, 7);
 #else
   (void)at, (void)v;
 #endif
@@ -428,13 +440,16 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   for (int it = 0; it < rounds; ++it) {
     const int pos = pos_of(it);
     const bool here = pos < last, more = it + 1 < rounds && pos_of(it + 1) < last;
-    if (more) {  // two stages under way while the older one is waited for
+    if constexpr (RG > 1) {  // everybody's share of this stage has come, and everybody is done with the one before
+      wait_loads<0>();
+      join_round();
+      if (more) request(pos_of(it + 1), (it + 1) & 1);
+    } else if (more) {  // two stages under way while the older one is waited for
       request(pos_of(it + 1), (it + 1) & 1);
       wait_loads<kStageLoads>();
     } else {
       wait_loads<0>();
     }
-    if (RG > 1) join_round();
     if (here) {
       const lds_char *const ks_lds = lds + (pg * Shape::kBuffers + (it & 1)) * Shape::kStage, *const vs_lds = ks_lds + Shape::kHalf;
       float16v sc[NT];
@@ -516,26 +531,26 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       uint32_t v_here[MD][2];
 #pragma unroll
       for (int m = 0; m < MD; ++m) v_here[m][0] = v_at[m][0] + vs_at, v_here[m][1] = v_at[m][1] + vs_at;
-      auto weigh = [&](auto nu) {  // 16 positions' products with their weights
-        constexpr int n = decltype(nu)::value / 2, u = decltype(nu)::value % 2;
-        short8v vf[MD];
-        read_transposed<n * (32 * DP * 2) + u * (16 * DP * 2)>(v_here, vf);
+      auto weigh = [&](auto nu) {  // 32 positions' products with their weights
+        constexpr int n = decltype(nu)::value;
+        short8v vf[2][MD];
+        read_transposed<n * (32 * DP * 2), 16 * DP * 2>(v_here, vf);
         if (odd[n]) {  // a weight of zero must not meet them: they are added by hand where the weight is not zero
 #pragma unroll
-          for (int m = 0; m < MD; ++m)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (special<T>((uint16_t)vf[m][e])) vf[m][e] = 0;
+            for (int m = 0; m < MD; ++m)
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (special<T>((uint16_t)vf[u][m][e])) vf[u][m][e] = 0;
         }
 #pragma unroll
-        for (int m = 0; m < MD; ++m) o[m] = mfma<T>(vf[m], pf[n][u], o[m]);
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int m = 0; m < MD; ++m) o[m] = mfma<T>(vf[u][m], pf[n][u], o[m]);
       };
       weigh(std::integral_constant<int, 0>());
-      weigh(std::integral_constant<int, 1>());
-      if constexpr (NT == 2) {
-        weigh(std::integral_constant<int, 2>());
-        weigh(std::integral_constant<int, 3>());
-      }
+      if constexpr (NT == 2) weigh(std::integral_constant<int, 1>());
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         for (uint32_t rest = odd[n]; rest; rest &= rest - 1) {
@@ -561,8 +576,6 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
           }
         }
     }
-    // The buffer is loaded into again in the next round.
-    if (RG > 1) join_round();
   }
   {
     const Halves both = halves(sum);
@@ -667,13 +680,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   if (bad_page && lane_id == 0) raise(a.status, PLC_ERR_INVALID);
 }
 
-constexpr int kJoinGroups = 4;
-// Joins the chunks of rows whose positions were cut: four components to a lane.
-template <class T>
+// Joins the chunks of rows whose positions were cut: four components to a lane, and kGroups groups of lanes that go through
+// the parts in turn, each with a maximum of its own, so that all loads of a batch are under way at once.
+constexpr int kJoinBatch = 8;
+template <class T, int kGroups>
 __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   __shared__ uint32_t line[kLineWords];
   __shared__ float4v meet_o[kBlock];
-  __shared__ float meet_l[kBlock];
+  __shared__ float2 meet_ml[kBlock];
+  constexpr int kLanes = kBlock / kGroups;
   const PoolView &p = a.p;
   bool bad = false;
   const Line mine = draw_line(a, line, &bad);
@@ -685,37 +700,51 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   const int parts = v.chunks;
   if (parts <= 1) return;
   const int64_t part0 = (int64_t)s_begin + (int64_t)blockIdx.x * parts;
-  // four groups of lanes take a quarter of the parts each
-  const int pieces = 2 * p.d8, i = (int)blockIdx.z * (kBlock / kJoinGroups) + (int)threadIdx.x % (kBlock / kJoinGroups);
-  const int group = (int)threadIdx.x / (kBlock / kJoinGroups);
+  const int pieces = 2 * p.d8, i = (int)blockIdx.z * kLanes + (int)threadIdx.x % kLanes, group = (int)threadIdx.x / kLanes;
   const int r = i / pieces, e = i % pieces * 4, row = row_tile * a.tile_rows + r;
   const bool here = r < a.tile_rows && row < v.t * a.G;
-  auto part = [&](int c) { return (part0 + c) * a.tile_rows + r; };
   float peak = kLowest, sums = 0.0f;
   float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (here) {
-#pragma unroll 8
-    for (int c = 0; c < parts; ++c) peak = fmaxf(peak, a.part_ml[2 * part(c)]);
-#pragma unroll 8
-    for (int c = group; c < parts; c += kJoinGroups) {
-      const float2 m = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(c));
-      const float4v x = *reinterpret_cast<const float4v *>(a.part_o + part(c) * (8 * p.d8) + e);
-      const float w = __builtin_amdgcn_exp2f(m.x - peak);
-      const bool any = m.y != 0.0f;  // (a part that has seen nothing has weight zero, not zero times what it holds)
-      sums += any ? w * m.y : 0.0f;
+  // (a part that has seen nothing has weight zero, not zero times what it holds)
+  auto add = [&](float2 m, float4v x, float now) {
+    const float w = __builtin_amdgcn_exp2f(m.x - now);
+    const bool any = m.y != 0.0f;
+    sums += any ? w * m.y : 0.0f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] += any ? w * x[k] : 0.0f;
+    for (int k = 0; k < 4; ++k) o[k] += any ? w * x[k] : 0.0f;
+  };
+  if (here) {
+    for (int c = group; c < parts; c += kGroups * kJoinBatch) {
+      float2 m[kJoinBatch];
+      float4v x[kJoinBatch];
+#pragma unroll
+      for (int u = 0; u < kJoinBatch; ++u) {
+        const int64_t part = (part0 + min(c + u * kGroups, parts - 1)) * a.tile_rows + r;
+        m[u] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part);
+        x[u] = *reinterpret_cast<const float4v *>(a.part_o + part * (8 * p.d8) + e);
+        if (c + u * kGroups >= parts) m[u] = make_float2(kLowest, 0.0f);
+      }
+      float now = peak;
+#pragma unroll
+      for (int u = 0; u < kJoinBatch; ++u) now = fmaxf(now, m[u].x);
+      const float keep = __builtin_amdgcn_exp2f(peak - now);
+      peak = now;
+      sums *= keep;
+      o *= keep;
+#pragma unroll
+      for (int u = 0; u < kJoinBatch; ++u) add(m[u], x[u], now);
     }
   }
   meet_o[threadIdx.x] = o;
-  meet_l[threadIdx.x] = sums;
+  meet_ml[threadIdx.x] = make_float2(peak, sums);
   __syncthreads();
   if (group != 0 || !here) return;
 #pragma unroll
-  for (int g = 1; g < kJoinGroups; ++g) {
-    o += meet_o[threadIdx.x + g * (kBlock / kJoinGroups)];
-    sums += meet_l[threadIdx.x + g * (kBlock / kJoinGroups)];
-  }
+  for (int g = 1; g < kGroups; ++g) peak = fmaxf(peak, meet_ml[threadIdx.x + g * kLanes].x);
+  sums = 0.0f;
+  o = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) add(meet_ml[threadIdx.x + g * kLanes], meet_o[threadIdx.x + g * kLanes], peak);
   const int node = v.n0 + row / a.G, head = h * a.G + row % a.G;
   const float scale = sums == 0.0f ? 0.0f : 1.0f / sums;
   *reinterpret_cast<ushort4 *>(a.out + node * a.out_node + head * a.out_head + e) =
@@ -803,11 +832,14 @@ int attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   if (d <= 64) launch_attend<T, 64>(a, plan, st);
   else if (d <= 128) launch_attend<T, 128>(a, plan, st);
   else launch_attend<T, 256>(a, plan, st);
-  const int64_t joined = (int64_t)a.max_nodes * a.G < plan.rows ? (int64_t)a.max_nodes * a.G : plan.rows;  // rows of a tile
-  if (plan.parts > 1)
-    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(plan.row_tiles * a.p.H), (unsigned)a.p.S,
-                                            (unsigned)((joined * 2 * a.p.d8 * kJoinGroups + kBlock - 1) / kBlock)),
+  if (plan.parts > 1) {
+    const int64_t joined = (int64_t)a.max_nodes * a.G < plan.rows ? (int64_t)a.max_nodes * a.G : plan.rows;  // rows of a tile
+    const int groups = plan.parts > 4 * kJoinBatch ? 16 : plan.parts > kJoinBatch ? 4 : 1;
+    const auto join = groups == 16 ? &join_kernel<T, 16> : groups == 4 ? &join_kernel<T, 4> : &join_kernel<T, 1>;
+    hipLaunchKernelGGL(join, dim3((unsigned)(plan.row_tiles * a.p.H), (unsigned)a.p.S,
+                                  (unsigned)((joined * 2 * a.p.d8 * groups + kBlock - 1) / kBlock)),
                        dim3(kBlock), 0, st, a);
+  }
   return launch_status();
 }
 
