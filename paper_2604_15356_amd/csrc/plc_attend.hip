@@ -40,7 +40,8 @@ constexpr int kLineWords = 1024 + 1;  // where each session begins on it
 struct AttendArgs {
   PoolView p;
   int32_t layer, G, max_nodes, max_len;
-  int32_t tile_rows, chunk;  // rows of a tile, positions of a chunk
+  int32_t tile_rows;  // rows of a tile
+  int32_t chunk;      // positions of a chunk; 0: the work at hand in equal parts, one for each compute unit
   int64_t N, q_node, q_head, out_node, out_head;
   const uint16_t *q;
   uint16_t *out;
@@ -54,10 +55,14 @@ struct AttendArgs {
 
 // A session as its part of the line: none where what is said of it cannot be (status tells), or it has no nodes.
 struct SessionView {
-  int32_t n0, t, len, row_tiles, chunks;  // first node, nodes, positions, tiles of rows, chunks of one tile and head
+  int32_t n0, t, len, row_tiles;  // first node, nodes, positions, tiles of rows
+  // chunks of one tile and head
+  __device__ __forceinline__ uint32_t chunks(uint32_t chunk) const { return row_tiles ? ((uint32_t)len + chunk - 1) / chunk : 0u; }
 };
-__device__ __forceinline__ SessionView session_of(const AttendArgs &a, int32_t n0, int32_t n1, int32_t len, bool *bad) {
-  SessionView v = {n0, n1 - n0, len, 0, 0};
+__device__ __forceinline__ SessionView session_of(const AttendArgs &a, int s, bool *bad) {
+  if (s >= a.p.S) return {};
+  const int32_t n0 = a.off[s], n1 = a.off[s + 1], len = a.p.lens[s];
+  SessionView v = {n0, n1 - n0, len, 0};
   if (v.t == 0) return v;
   if (v.t < 0 || n0 < 0 || n1 > a.N || v.t > a.max_nodes || len < v.t || len > a.max_len ||
       len > ((int64_t)a.p.M << a.p.shift)) {
@@ -65,28 +70,38 @@ __device__ __forceinline__ SessionView session_of(const AttendArgs &a, int32_t n
     return v;
   }
   v.row_tiles = (v.t * a.G + a.tile_rows - 1) / a.tile_rows;
-  v.chunks = (int32_t)(((uint32_t)len + (uint32_t)a.chunk - 1) / (uint32_t)a.chunk);
   return v;
 }
 
 // Where each session begins on the line, which ends at `total` (below 2^31: checked on the host).  Up to 64 sessions every
 // wavefront holds for itself, a lane each; more are written down in LDS, line[S] being the total.
+constexpr uint32_t kUnit = 128;  // a chunk's positions are a multiple
 struct Line {
-  uint32_t begin, total;
-  int32_t n0, t, len;
+  uint32_t begin, total, chunk;
+  SessionView v;
 };
 __device__ __forceinline__ Line draw_line(const AttendArgs &a, uint32_t *line, bool *bad) {
   const int lane = threadIdx.x & 63;
-  Line mine = {};
+  const auto last_of = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); };
+  const SessionView v0 = session_of(a, lane, bad);
+  uint32_t chunk = (uint32_t)a.chunk;
+  if (chunk == 0) {  // (fewer than 256 tiles and heads, of less than 2^23 units each)
+    uint32_t units = 0;
+    for (int s0 = 0; s0 < a.p.S; s0 += 64) {
+      const SessionView v = s0 == 0 ? v0 : session_of(a, s0 + lane, bad);
+      units += last_of(wave_inclusive_scan((uint32_t)v.row_tiles * v.chunks(kUnit) * (uint32_t)a.p.H));
+    }
+    chunk = units <= kComputeUnits ? kUnit : (units + kComputeUnits - 1) / kComputeUnits * kUnit;
+  }
+  Line mine = {0u, 0u, chunk, v0};
   uint32_t at = 0;
   for (int s0 = 0; s0 < a.p.S; s0 += 64) {
     const int s = s0 + lane;
-    SessionView v = {};
-    if (s < a.p.S) v = session_of(a, a.off[s], a.off[s + 1], a.p.lens[s], bad);
-    const uint32_t n = (uint32_t)(v.row_tiles * v.chunks) * (uint32_t)a.p.H, upto = wave_inclusive_scan(n);
-    mine = {at + upto - n, 0, v.n0, v.t, v.len};
+    const SessionView v = s0 == 0 ? v0 : session_of(a, s, bad);
+    const uint32_t n = (uint32_t)v.row_tiles * v.chunks(chunk) * (uint32_t)a.p.H, upto = wave_inclusive_scan(n);
+    mine.begin = at + upto - n;
     if (a.p.S > 64 && threadIdx.x < 64 && s < a.p.S) line[s] = mine.begin;
-    at += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    at += last_of(upto);
   }
   if (a.p.S > 64) {
     if (threadIdx.x == 0) line[a.p.S] = at;
@@ -243,7 +258,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     if (bad && id == 0) raise(a.status, PLC_ERR_INVALID);
   }
   const auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-  const uint32_t total = scalar(mine.total);
+  const uint32_t total = scalar(mine.total), chunk = scalar(mine.chunk);
   bool bad_page = false;
 
   for (uint32_t at = blockIdx.x; at < total; at += gridDim.x) {
@@ -258,7 +273,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   if (p.S <= 64) {
     s = __builtin_popcountll(__ballot(lane < p.S && mine.begin <= at)) - 1;
     s_begin = (uint32_t)__builtin_amdgcn_readlane((int)mine.begin, s);
-    n0 = __builtin_amdgcn_readlane(mine.n0, s), t = __builtin_amdgcn_readlane(mine.t, s), len = __builtin_amdgcn_readlane(mine.len, s);
+    n0 = __builtin_amdgcn_readlane(mine.v.n0, s), t = __builtin_amdgcn_readlane(mine.v.t, s), len = __builtin_amdgcn_readlane(mine.v.len, s);
   } else {
     s = -1;
     for (int s0 = 0; s0 < p.S; s0 += 64)
@@ -267,15 +282,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     const const_int *const off = (const const_int *)a.off;
     n0 = off[s], t = off[s + 1] - n0, len = ((const const_int *)p.lens)[s];
   }
-  const uint32_t chunks = scalar(((uint32_t)len + (uint32_t)a.chunk - 1) / (uint32_t)a.chunk);
+  const uint32_t chunks = scalar(((uint32_t)len + chunk - 1) / chunk);
   const uint32_t pair = scalar((at - s_begin) / chunks), nth = at - s_begin - pair * chunks;
   const int row_tile = (int)scalar(pair / (uint32_t)p.H), h = (int)pair - row_tile * p.H;
   const bool whole = chunks == 1;
 
   const int R = t * a.G, r0 = row_tile * Shape::kRows;
-  const int first = (int)nth * a.chunk, ctx = len - t;
+  const int first = (int)(nth * chunk), ctx = len - t;
   const bool chain = a.parents == nullptr;
-  int last = min(len - first, a.chunk) + first;
+  int last = (int)min((uint32_t)(len - first), chunk) + first;
   if (chain) last = min(last, ctx + (int)scalar((uint32_t)(min(R, r0 + Shape::kRows) - 1) / (uint32_t)a.G) + 1);  // what the tile's last node sees
 
   // this lane's row
@@ -694,10 +709,10 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   const Line mine = draw_line(a, line, &bad);
   const int s = (int)blockIdx.y;
   const uint32_t s_begin = p.S <= 64 ? (uint32_t)__builtin_amdgcn_readlane((int)mine.begin, s) : line[s];
-  const SessionView v = session_of(a, a.off[s], a.off[s + 1], p.lens[s], &bad);
+  const SessionView v = session_of(a, s, &bad);
   const int row_tile = (int)blockIdx.x / p.H, h = (int)blockIdx.x % p.H;
   if (row_tile >= v.row_tiles) return;
-  const int parts = v.chunks;
+  const int parts = (int)v.chunks(mine.chunk);
   if (parts <= 1) return;
   const int64_t part0 = (int64_t)s_begin + (int64_t)blockIdx.x * parts;
   const int pieces = 2 * p.d8, i = (int)blockIdx.z * kLanes + (int)threadIdx.x % kLanes, group = (int)threadIdx.x / kLanes;
@@ -757,8 +772,8 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
 
 struct AttendPlan {
   int rows;                        // of a tile
-  int32_t chunk;                   // positions
-  int64_t row_tiles, parts, line;  // tiles of a session, chunks of a tile and head, chunks of all: at most
+  int32_t chunk;                   // positions; 0: set by the work at hand
+  int64_t row_tiles, parts, line;  // tiles of a session, chunks of a tile and head (as far as is known here), chunks of all: at most
 };
 
 constexpr int64_t kMostGroups = 2048;  // workgroups: bounds from the host may be far above what there is to do
@@ -768,26 +783,29 @@ constexpr int64_t kPartRows = 131072;  // rows of partial results, at most, that
 AttendPlan attend_plan(const plc_pages *p, int32_t G, int32_t max_nodes, int32_t max_len) {
   AttendPlan plan;
   const int64_t rows = (int64_t)max_nodes * G;
-  const bool wide = p->d > 128;
-  plan.rows = rows <= 32 ? 32 : rows <= 64 || wide ? 64 : 128;
+  plan.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   plan.row_tiles = (rows + plan.rows - 1) / plan.rows;
   const int64_t pairs = plan.row_tiles * p->H * p->S;
-  // A chunk is a workgroup's work.  Whole positions of a tile of rows and head need no joining (a launch, 5 us), and where
-  // there is one for every compute unit nothing is gained by cutting them: 64 sessions x 8 heads of up to 4000 positions
-  // 108 us, cut in two 121 us.  Fewer are cut until there are as many chunks as the chip holds workgroups, one a compute
-  // unit for a single tile of 32 rows, two for more: one session of 16,000 positions 20 us, in twice as many chunks 28 us.
-  // Short ones are quicker done by one workgroup (500 positions 7.7 against 10.1 us, 1000 positions 10.8 against 9.8).
+  // A chunk is a workgroup's work, and a workgroup's LDS a compute unit's.  Whole positions of a tile of rows and head need no
+  // joining (a launch, 5 us), and where there is one for every compute unit nothing is gained by cutting them: 64 sessions x 8
+  // heads of up to 4000 positions 108 us, cut in two 121 us.  Fewer are cut into as many chunks as there are compute units, of
+  // a length that the kernels find from the sessions' own.  Short ones are quicker done by one workgroup (500 positions 7.7
+  // against 10.1 us, 1000 positions 10.8 against 9.8).
+  const int64_t enough = plan.rows == 32 ? 768 : 384;
+  if (max_len > (2 * pairs > kComputeUnits ? 1536 : enough) && pairs < kComputeUnits) {
+    plan.chunk = 0;
+    plan.parts = (kComputeUnits + pairs - 1) / pairs;
+    plan.line = kComputeUnits + pairs;  // a tile and head's last chunk may be short
+    return plan;
+  }
   int64_t chunk = max_len;
-  const bool small = plan.rows == 32;
-  if (max_len > (small ? 768 : 384)) {
-    const int64_t target = small ? kComputeUnits : 2 * kComputeUnits;
-    if (pairs < kComputeUnits) chunk = (max_len * pairs + target - 1) / target;
-    chunk = chunk > kLongest ? kLongest : chunk;
+  if (max_len > enough) {
     const int64_t most = kPartRows / plan.rows / pairs;  // parts
+    chunk = chunk > kLongest ? kLongest : chunk;
     if (most < 2) chunk = max_len;
     else if (chunk * most < max_len) chunk = (max_len + most - 1) / most;
   }
-  plan.chunk = (int32_t)(chunk > INT32_MAX - 128 ? INT32_MAX - 127 : (chunk + 127) / 128 * 128);
+  plan.chunk = (int32_t)(chunk > INT32_MAX - (int64_t)kUnit ? INT32_MAX - (int64_t)kUnit + 1 : (chunk + kUnit - 1) / kUnit * kUnit);
   plan.parts = (max_len + (int64_t)plan.chunk - 1) / plan.chunk;
   plan.line = pairs > INT32_MAX ? INT64_MAX : pairs * plan.parts;
   return plan;
@@ -818,11 +836,12 @@ template <class T, int DP>
 void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   if constexpr (DP <= 128) {
     if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 4, 1>>(a, plan, st);
-    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, plan, st);
-    else launch_attend<T, AttendShape<DP, 4, 1, 2>>(a, plan, st);
+    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 4, 1>>(a, plan, st);
+    else launch_attend<T, AttendShape<DP, 4, 2, 2>>(a, plan, st);
   } else {
     if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, plan, st);
-    else launch_attend<T, AttendShape<DP, 2, 1, 1>>(a, plan, st);
+    else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, plan, st);
+    else launch_attend<T, AttendShape<DP, 4, 1, 1>>(a, plan, st);
   }
 }
 
