@@ -9,12 +9,18 @@
 // to come in that same order, which two transposing LDS reads of 4 positions x 16 components give.
 //
 // Inside a workgroup the wavefronts form RG groups of 32 rows that share what is loaded, and PG groups that take turns with
-// the positions: a step of one token with few rows has two wavefronts on positions of their own and no barrier, a large tree
-// has four times 32 rows on the same positions.
+// the positions: a step of one token with few rows has up to four wavefronts on positions of their own and no barrier, a
+// large tree has four times 32 rows on the same positions (launch_attend has the rule).
 //
 // The work is a line of chunks: session after session, in each its tiles of rows and heads, in each of those its positions,
 // cut where they are long, or where there are few rows and heads to fill the chip with (attend_plan has the rule).
 // Workgroups take the chunks in turn; what a cut has split is joined by a second kernel.
+//
+// What bounds it: few rows, HBM (64 sessions of one token, 8 heads, 4 query heads each, up to 4096 positions: 545 MB in 112 us,
+// 4.9 TB/s; a large copy reaches 4.9); many rows, the turns of the matrix cores and the vector units (64 nodes, 32,768
+// positions: 34 GFLOP in 57 us with the joining, 0.60 PFLOP/s; the matrix cores are busy a third of the time, the softmax and
+// its waits take the rest); short contexts, the 4 us from a workgroup's start to its first products (offsets, table, pages,
+// one after the other) and 3.5 us of its end.
 #include <type_traits>
 
 #include "plc_device.h"
@@ -834,12 +840,22 @@ void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) 
 
 template <class T, int DP>
 void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
+  // A workgroup that fills a compute unit's LDS leaves fewer partial results, and more of it is under way for one tile and
+  // head (64 sessions of 8 heads, up to 4096 positions: 112 against 120 us).  Where there are several tiles and heads for each
+  // compute unit, two workgroups of half the size hide each other's beginnings and ends: 20 sessions of 64 heads and 243
+  // positions 37 against 48 us, 64 sessions of 16 heads with trees of up to 27 nodes over up to 500 positions 56 against 81 us.
+  const bool many = plan.line >= 4 * kComputeUnits;
   if constexpr (DP <= 128) {
-    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 4, 1>>(a, plan, st);
+    if (plan.rows == 32 && many) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, plan, st);
+    else if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 4, 1>>(a, plan, st);
+    else if (plan.rows == 64 && many) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, plan, st);
     else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 4, 1>>(a, plan, st);
+    else if (many) launch_attend<T, AttendShape<DP, 4, 1, 2>>(a, plan, st);
     else launch_attend<T, AttendShape<DP, 4, 2, 2>>(a, plan, st);
   } else {
-    if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, plan, st);
+    if (plan.rows == 32 && many) launch_attend<T, AttendShape<DP, 1, 1, 1>>(a, plan, st);
+    else if (plan.rows == 32) launch_attend<T, AttendShape<DP, 1, 2, 1>>(a, plan, st);
+    else if (plan.rows == 64 && many) launch_attend<T, AttendShape<DP, 2, 1, 1>>(a, plan, st);
     else if (plan.rows == 64) launch_attend<T, AttendShape<DP, 2, 2, 1>>(a, plan, st);
     else launch_attend<T, AttendShape<DP, 4, 1, 1>>(a, plan, st);
   }

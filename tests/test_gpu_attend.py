@@ -150,6 +150,21 @@ def test_long_contexts_are_joined_from_chunks(dtype, n, t, G):
     check(dtype, 128, G, 1, 16, [n, 700, t], [t, t, t], True, seed=n + t)
 
 
+@pytest.mark.parametrize("d", [64, 96, 256])
+@pytest.mark.parametrize("G,t", [(2, 3), (20, 2), (40, 2)])
+def test_many_tiles_and_heads(d, G, t):
+    """Several tiles and heads for each compute unit: the smaller workgroups, each of their arrangements."""
+    lens = [t + 5 * i for i in range(16)]
+    check(torch.bfloat16, d, G, 64, 16, lens, [t] * 16, True, seed=d + G)
+
+
+@pytest.mark.parametrize("lens", [[17 * i + 1 for i in range(100)], [9] * 70 + [5000], [1601 - 8 * i for i in range(200)],
+                                  [20000] + [3] * 59])
+def test_chunks_follow_the_sessions_lengths(lens):
+    """Contexts of which the host knows the longest only: many sessions, one long one among short ones."""
+    check(torch.float16, 64, 2, 1, 16, lens, [1 + (i % 2) * (n > 1) for i, n in enumerate(lens)], True, seed=len(lens))
+
+
 def test_strides_layers_and_scales():
     for layer in range(3):
         check(torch.float16, 80, 2, 3, 16, [50, 7], [5, 7], True, seed=layer, layout="gaps", L=3, layer=layer, scale=0.3)
