@@ -13,6 +13,51 @@ namespace {
 
 constexpr int kManager = 1024;  // threads of the one workgroup that hands out pages; as many sessions at most
 
+// ---- 16 bytes at a time ------------------------------------------------------------------------------------------------
+
+// 16 bytes of a row.  Past the caches (kStream) where more is stored than they hold: 1.07 GB in and out 195 us, through them
+// 208 us, 134 MB 24.9 against 28.8 us; but 67 MB, there from the call before, 14.2 against 12.3 us.  Rows that are loaded gain
+// nothing by it (537 MB 114 against 110 us), and the encoder reads them next.
+template <bool kStream>
+__device__ __forceinline__ uint4 get16(const uint16_t *p) {
+  return kStream ? load16_stream(p) : *reinterpret_cast<const uint4 *>(p);
+}
+template <bool kStream>
+__device__ __forceinline__ void put16(uint16_t *p, uint4 v) {
+  if (kStream) store16_stream(p, v);
+  else *reinterpret_cast<uint4 *>(p) = v;
+}
+
+// The first `rows` rows of a page's heads slab, slab + step, ... (of both halves) from one page to another.
+template <bool kStream, int kThreads>
+__device__ __forceinline__ void copy_slabs(const PoolView &p, int64_t from, int64_t to, int32_t rows, int32_t slab0,
+                                           int32_t slab1) {
+  const int32_t items = rows * p.d8;
+  const bool dense = p.row_s == (int64_t)p.d8 * 8;
+  for (int32_t i = threadIdx.x; i < items; i += kThreads) {
+    const int64_t in_slab = dense ? (int64_t)i * 8 : (i / p.d8) * p.row_s + (int64_t)(i % p.d8) * 8;
+    for (int32_t slab = slab0; slab < slab1; slab += 4) {
+      uint4 k[4], v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int32_t lh = min(slab + u, slab1 - 1);
+        const int64_t at = from * p.page_s + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + in_slab;
+        k[u] = get16<kStream>(p.k + at);
+        v[u] = get16<kStream>(p.v + at);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int32_t lh = slab + u;
+        if (lh < slab1) {
+          const int64_t at = to * p.page_s + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + in_slab;
+          put16<kStream>(p.k + at, k[u]);
+          put16<kStream>(p.v + at, v[u]);
+        }
+      }
+    }
+  }
+}
+
 // ---- bookkeeping ------------------------------------------------------------------------------------------------------
 
 // Exclusive prefix sum over the 1024 threads of a workgroup.  `smem`: 17 words.
@@ -99,10 +144,13 @@ __global__ __launch_bounds__(kBlock) void fork_kernel(PoolView p, const int32_t 
 }
 
 // Pages for the sessions' new positions, a thread per session: the list of tail pages to copy, and the pages taken, in order.
+// kCopies: the tails are so small that this workgroup copies them too (4 beams, pages of 32 KB: 5.4 us where two kernels took
+// 6.6 and 2.9, and a launch less for the host).
 struct CopyList {
   uint32_t count, pad[3];
   int32_t from[kManager], to[kManager], rows[kManager];
 };
+template <bool kCopies>
 __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int32_t *__restrict__ grow,
                                                           CopyList *__restrict__ copies, int32_t *__restrict__ taken,
                                                           uint32_t *status) {
@@ -193,16 +241,22 @@ __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int3
     atomicSub(&p.refs[tail], 1);
   }
   if (g > 0) p.lens[s] = (int32_t)(len + g);
+  if (kCopies) {
+    __syncthreads();
+    for (uint32_t i = 0; i < n_copies; ++i)
+      copy_slabs<false, kManager>(p, copies->from[i], copies->to[i], copies->rows[i], 0, p.L * p.H);
+  }
 }
 
 // One workgroup per session gives back the pages behind its new length.
+template <int kThreads>
 __device__ __forceinline__ void trim_session(const PoolView &p, int32_t s, int64_t now, uint32_t *status) {
   const int64_t was = p.lens[s];
   if (was < 0 || was > ((int64_t)p.M << p.shift) || now < 0 || now > was) {
     if (threadIdx.x == 0) raise(status, PLC_ERR_INVALID);
     return;
   }
-  for (int32_t j = pages_of(now, p.shift) + (int32_t)threadIdx.x; j < pages_of(was, p.shift); j += kBlock) {
+  for (int32_t j = pages_of(now, p.shift) + (int32_t)threadIdx.x; j < pages_of(was, p.shift); j += kThreads) {
     int32_t *const entry = &p.table[(int64_t)s * p.M + j];
     const int32_t page = *entry;
     *entry = -1;
@@ -214,7 +268,7 @@ __device__ __forceinline__ void trim_session(const PoolView &p, int32_t s, int64
 }
 
 __global__ __launch_bounds__(kBlock) void trim_kernel(PoolView p, const int32_t *__restrict__ new_lens, uint32_t *status) {
-  trim_session(p, (int32_t)blockIdx.x, new_lens[blockIdx.x], status);
+  trim_session<kBlock>(p, (int32_t)blockIdx.x, new_lens[blockIdx.x], status);
 }
 
 // The nodes of a session's tree that are kept: checked, as both kernels of plc_pages_accept need them.
@@ -237,7 +291,7 @@ __global__ __launch_bounds__(kBlock) void accept_trim_kernel(PoolView p, const i
                                                              const int32_t *__restrict__ path_off, int64_t path_len,
                                                              uint32_t *status) {
   const Accepted a = accepted_of(p, (int32_t)blockIdx.x, off, path_off, path_len);
-  if (a.ok) trim_session(p, (int32_t)blockIdx.x, a.ctx + a.m, status);
+  if (a.ok) trim_session<kBlock>(p, (int32_t)blockIdx.x, a.ctx + a.m, status);
   else if (threadIdx.x == 0) raise(status, PLC_ERR_INVALID);
 }
 
@@ -273,56 +327,13 @@ __global__ __launch_bounds__(kManager) void compact_kernel(PoolView p, MoveList 
 
 // ---- rows ---------------------------------------------------------------------------------------------------------------
 
-// 16 bytes of a row.  Past the caches (kStream) where more is stored than they hold: 1.07 GB in and out 195 us, through them
-// 208 us, 134 MB 24.9 against 28.8 us; but 67 MB, there from the call before, 14.2 against 12.3 us.  Rows that are loaded gain
-// nothing by it (537 MB 114 against 110 us), and the encoder reads them next.
-template <bool kStream>
-__device__ __forceinline__ uint4 get16(const uint16_t *p) {
-  return kStream ? load16_stream(p) : *reinterpret_cast<const uint4 *>(p);
-}
-template <bool kStream>
-__device__ __forceinline__ void put16(uint16_t *p, uint4 v) {
-  if (kStream) store16_stream(p, v);
-  else *reinterpret_cast<uint4 *>(p) = v;
-}
-
-// The first `rows` rows of a page's heads slab, slab + step, ... (of both halves) from one page to another.
-template <bool kStream>
-__device__ __forceinline__ void copy_slabs(const PoolView &p, int64_t from, int64_t to, int32_t rows, int32_t slab0,
-                                           int32_t slab1) {
-  const int32_t items = rows * p.d8;
-  const bool dense = p.row_s == (int64_t)p.d8 * 8;
-  for (int32_t i = threadIdx.x; i < items; i += kBlock) {
-    const int64_t in_slab = dense ? (int64_t)i * 8 : (i / p.d8) * p.row_s + (int64_t)(i % p.d8) * 8;
-    for (int32_t slab = slab0; slab < slab1; slab += 4) {
-      uint4 k[4], v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int32_t lh = min(slab + u, slab1 - 1);
-        const int64_t at = from * p.page_s + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + in_slab;
-        k[u] = get16<kStream>(p.k + at);
-        v[u] = get16<kStream>(p.v + at);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int32_t lh = slab + u;
-        if (lh < slab1) {
-          const int64_t at = to * p.page_s + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + in_slab;
-          put16<kStream>(p.k + at, k[u]);
-          put16<kStream>(p.v + at, v[u]);
-        }
-      }
-    }
-  }
-}
-
 constexpr int kSlabs = 4;  // heads of a page that a workgroup copies at a time
 
 __global__ __launch_bounds__(kBlock) void copy_tails_kernel(PoolView p, const CopyList *__restrict__ copies) {
   const uint32_t i = blockIdx.y;
   if (i >= copies->count) return;
   const int32_t slab = (int32_t)blockIdx.x * kSlabs, slabs = p.L * p.H;
-  copy_slabs<false>(p, copies->from[i], copies->to[i], copies->rows[i], slab, min(slab + kSlabs, slabs));
+  copy_slabs<false, kBlock>(p, copies->from[i], copies->to[i], copies->rows[i], slab, min(slab + kSlabs, slabs));
 }
 
 // The first `table_blocks` workgroups rewrite the tables, the others copy pages.
@@ -349,7 +360,7 @@ __global__ __launch_bounds__(kBlock) void move_pages_kernel(PoolView p, const Mo
   const int64_t units = (int64_t)count * per_page;
   for (int64_t u = (int32_t)blockIdx.x - table_blocks; u < units; u += (int32_t)gridDim.x - table_blocks) {
     const int32_t i = (int32_t)(u / per_page), slab = (int32_t)(u % per_page) * kSlabs;
-    copy_slabs<true>(p, movers[i], holes[i], 1 << p.shift, slab, min(slab + kSlabs, slabs));
+    copy_slabs<true, kBlock>(p, movers[i], holes[i], 1 << p.shift, slab, min(slab + kSlabs, slabs));
   }
 }
 
@@ -357,15 +368,13 @@ __global__ __launch_bounds__(kBlock) void move_pages_kernel(PoolView p, const Mo
 // order, several nodes at a time, all of their loads before the first of their stores: a row goes only to places whose own
 // node has been read (path[r] >= r, ascending).
 constexpr int kPathRound = 64, kPathBatch = 8;
-__global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const int32_t *__restrict__ off,
-                                                             const int32_t *__restrict__ path, int64_t path_len,
-                                                             const int32_t *__restrict__ path_off, uint32_t *status) {
-  __shared__ int64_t from[kPathRound], to[kPathRound];
-  const int32_t s = (int32_t)blockIdx.y;
-  const Accepted a = accepted_of(p, s, off, path_off, path_len);
-  if (!a.ok) return;  // the trimming kernel says so
+struct PathPlaces {
+  int64_t from[kPathRound], to[kPathRound];
+};
+template <int kThreads>
+__device__ __forceinline__ void accept_rows(const PoolView &p, int32_t s, const Accepted &a, const int32_t *path, int32_t i,
+                                            PathPlaces *places, uint32_t *status) {
   const int32_t columns = 2 * p.L * p.H * p.d8;
-  const int32_t i = (int32_t)blockIdx.x * kBlock + threadIdx.x;
   const int32_t c = i % p.d8, lh = i / p.d8 % (p.L * p.H);
   uint16_t *const base = (i < columns / 2 ? p.k : p.v) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)c * 8;
   for (int32_t r0 = 0; r0 < a.m; r0 += kPathRound) {
@@ -390,8 +399,8 @@ __global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const i
           }
         }
       }
-      from[threadIdx.x] = f;
-      to[threadIdx.x] = t;
+      places->from[threadIdx.x] = f;
+      places->to[threadIdx.x] = t;
     }
     __syncthreads();
     if (i < columns) {
@@ -399,13 +408,39 @@ __global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const i
         uint4 row[kPathBatch];
 #pragma unroll
         for (int u = 0; u < kPathBatch; ++u)
-          if (from[b + u] >= 0) row[u] = get16<false>(base + from[b + u]);
+          if (places->from[b + u] >= 0) row[u] = get16<false>(base + places->from[b + u]);
 #pragma unroll
         for (int u = 0; u < kPathBatch; ++u)
-          if (from[b + u] >= 0) put16<false>(base + to[b + u], row[u]);
+          if (places->from[b + u] >= 0) put16<false>(base + places->to[b + u], row[u]);
       }
     }
   }
+}
+
+__global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const int32_t *__restrict__ off,
+                                                             const int32_t *__restrict__ path, int64_t path_len,
+                                                             const int32_t *__restrict__ path_off, uint32_t *status) {
+  __shared__ PathPlaces places;
+  const int32_t s = (int32_t)blockIdx.y;
+  const Accepted a = accepted_of(p, s, off, path_off, path_len);
+  if (!a.ok) return;  // the trimming kernel says so
+  accept_rows<kBlock>(p, s, a, path, (int32_t)blockIdx.x * kBlock + (int32_t)threadIdx.x, &places, status);
+}
+
+// Both at once, for a single session of rows so short that one workgroup has them: a launch less.  (Of several sessions one
+// could give back a page while another looks whether it is its own.)
+__global__ __launch_bounds__(kManager) void accept_kernel(PoolView p, const int32_t *__restrict__ off,
+                                                          const int32_t *__restrict__ path, int64_t path_len,
+                                                          const int32_t *__restrict__ path_off, uint32_t *status) {
+  __shared__ PathPlaces places;
+  const Accepted a = accepted_of(p, 0, off, path_off, path_len);
+  if (!a.ok) {
+    if (threadIdx.x == 0) raise(status, PLC_ERR_INVALID);
+    return;
+  }
+  for (int32_t i = 0; i < 2 * p.L * p.H * p.d8; i += kManager) accept_rows<kManager>(p, 0, a, path, i + (int32_t)threadIdx.x, &places, status);
+  __syncthreads();
+  trim_session<kManager>(p, 0, a.ctx + a.m, status);
 }
 
 // Rows between a caller's buffer and pages.  A workgroup takes a block of consecutive rows, as many as give each thread 16
@@ -498,6 +533,7 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, co
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
 
+constexpr int64_t kFewBytes = 256 << 10;  // that one workgroup may copy
 constexpr int64_t kCached = (int64_t)96 << 20;  // bytes moved, in and out
 
 size_t copy_list_bytes() { return align_up(sizeof(CopyList), 256); }
@@ -560,7 +596,12 @@ extern "C" int plc_pages_extend(const plc_pages *pages, const int32_t *grow, voi
   const hipStream_t st = static_cast<hipStream_t>(stream);
   CopyList *const copies = static_cast<CopyList *>(ws);
   int32_t *const taken = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + copy_list_bytes());
-  hipLaunchKernelGGL(extend_kernel, dim3(1), dim3(kManager), 0, st, p, grow, copies, taken, status);
+  const int64_t tails = (int64_t)p.S * p.L * p.H << p.shift;  // rows, of 16 d8 bytes in each half
+  if (tails * p.d8 * 32 <= kFewBytes) {
+    hipLaunchKernelGGL(extend_kernel<true>, dim3(1), dim3(kManager), 0, st, p, grow, copies, taken, status);
+    return launch_status();
+  }
+  hipLaunchKernelGGL(extend_kernel<false>, dim3(1), dim3(kManager), 0, st, p, grow, copies, taken, status);
   hipLaunchKernelGGL(copy_tails_kernel, dim3((unsigned)((p.L * p.H + kSlabs - 1) / kSlabs), (unsigned)p.S), dim3(kBlock), 0, st,
                      p, copies);
   return launch_status();
@@ -581,6 +622,10 @@ extern "C" int plc_pages_accept(const plc_pages *pages, const int32_t *off, cons
   const PoolView p = pool_view(pages);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t columns = (int64_t)2 * p.L * p.H * p.d8;
+  if (p.S == 1 && columns <= 2 * kManager) {
+    hipLaunchKernelGGL(accept_kernel, dim3(1), dim3(kManager), 0, st, p, off, path, path_len, path_off, status);
+    return launch_status();
+  }
   if (path_len > 0)
     hipLaunchKernelGGL(accept_rows_kernel, dim3((unsigned)((columns + kBlock - 1) / kBlock), (unsigned)p.S), dim3(kBlock), 0,
                        st, p, off, path, path_len, path_off, status);

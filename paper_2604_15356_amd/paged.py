@@ -126,9 +126,9 @@ class PagedKVCache:
         if parents is not None:
             self._per_session(parents, N, "parents")
         if out is None:
-            out = q.new_empty((N, heads, self.d))
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if lse is None:
-            lse = q.new_empty((N, heads), dtype=torch.float32)
+            lse = torch.empty(N, heads, dtype=torch.float32, device=self.device)
         elif lse.shape != (N, heads):
             raise ValueError("lse is [nodes, heads]")
         if N == 0:

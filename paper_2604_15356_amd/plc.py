@@ -552,16 +552,17 @@ def plc_pages_workspace_bytes(pages) -> int:
 # plain addresses, and the stream is asked for directly.
 _I64x2 = C.c_int64 * 2
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_int32 = torch.int32
 
 
 def _ints(t):
-    if t.dtype is not torch.int32:
+    if t.dtype is _int32 and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not _int32:
         raise TypeError(f"expected {torch.int32}, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError("plc takes device tensors")
-    if not t.is_contiguous():
-        raise ValueError("tensor must be contiguous")
-    return t.data_ptr()
+    raise ValueError("tensor must be contiguous")
 
 
 def _on_device(t):
@@ -596,14 +597,24 @@ def plc_pages_compact(pages, used, ws, status):
                                    _raw_stream(ws.device.index)), "plc_pages_compact")
 
 
+_rows_known = {}  # descriptions of rows by their layout
+
+
 def _rows_of(k, v, layer):
     """Rows in a buffer: packed [rows, layers, heads, d], or [S, layers, heads, rows, d], of any strides but the last."""
     st, shape = k.stride(), k.shape
-    if shape != v.shape or k.dtype is not v.dtype or st != v.stride() or st[-1] != 1 or len(shape) not in (4, 5):
+    if shape != v.shape or k.dtype is not v.dtype or st != v.stride():
         raise ValueError("k and v are [rows, layers, heads, d] or [sessions, layers, heads, rows, d] of one layout")
-    if len(shape) == 4:
-        return plc_rows(layer, shape[1], 1, shape[0], (0, st[1], st[2], st[0]))
-    return plc_rows(layer, shape[1], 0, shape[3], st[:4])
+    rows = _rows_known.get((shape, st, layer))
+    if rows is None:
+        if len(shape) not in (4, 5) or st[-1] != 1:
+            raise ValueError("k and v are [rows, layers, heads, d] or [sessions, layers, heads, rows, d] of one layout")
+        if len(_rows_known) >= 1024:
+            _rows_known.clear()
+        rows = plc_rows(layer, shape[1], 1, shape[0], (0, st[1], st[2], st[0])) if len(shape) == 4 else \
+            plc_rows(layer, shape[1], 0, shape[3], st[:4])
+        _rows_known[shape, st, layer] = rows
+    return rows
 
 
 def plc_pages_store(pages, off, k, v, layer, status):
