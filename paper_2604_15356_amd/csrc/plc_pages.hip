@@ -78,22 +78,28 @@ __device__ __forceinline__ uint32_t manager_scan(uint32_t v, uint32_t *smem, uin
   return smem[wave] + inc - v;
 }
 
-// Walks all pages in order, eight to a thread and round (one load each, so that a round of 8192 pages is one trip to
-// memory): visit(page, rank) for every page that `is` holds for, `rank` counting them from 0.  Stops once `enough` are
-// found.  Returns how many there were up to there.
-constexpr int kScanWords = 8;
-template <class Is, class Visit>
-__device__ __forceinline__ uint32_t scan_pages(const int32_t *refs, int32_t first, int32_t last, uint32_t enough,
-                                               uint32_t *smem, const Is &is, const Visit &visit) {
-  uint32_t found = 0;
-  for (int64_t base = first; base < last && found < enough; base += kManager * kScanWords) {
-    uint32_t mine = 0;
-    // consecutive pages to consecutive threads' runs of eight
-    const int64_t p0 = base + (int64_t)threadIdx.x * kScanWords;
+// Which of the eight pages from p0 on are in use.
+constexpr int kScanWords = 8, kScanRound = kManager * kScanWords;
+__device__ __forceinline__ uint32_t used_bits(const PoolView &p, int64_t p0) {
+  uint32_t bits = 0;
 #pragma unroll
-    for (int j = 0; j < kScanWords; ++j)
-      if (p0 + j < last && is(refs[p0 + j])) mine |= 1u << j;
-    uint32_t total;
+  for (int j = 0; j < kScanWords; ++j)
+    if (p0 + j < p.P && p.refs[p0 + j] != 0) bits |= 1u << j;
+  return bits;
+}
+
+// Walks the pages [first, last) in order, eight to a thread and round (one load each, so that a round of 8192 pages is one trip
+// to memory, and `ready`, the first round's, can be asked for long before): visit(page, rank) for every page that is in use
+// (or is not), `rank` counting them from 0.  Stops once `enough` are found.  Returns how many there were up to there.
+template <class Visit>
+__device__ __forceinline__ uint32_t scan_pages(const PoolView &p, int32_t first, int32_t last, bool in_use, uint32_t ready,
+                                               uint32_t enough, uint32_t *smem, const Visit &visit) {
+  uint32_t found = 0;
+  for (int64_t base = first / kScanRound * kScanRound; base < last && found < enough; base += kScanRound) {
+    const int64_t p0 = base + (int64_t)threadIdx.x * kScanWords;
+    const uint32_t used = base == 0 ? ready : used_bits(p, p0);
+    const int lo = (int)max((int64_t)0, min((int64_t)kScanWords, first - p0)), hi = (int)max((int64_t)0, min((int64_t)kScanWords, last - p0));
+    uint32_t mine = (in_use ? used : ~used) & ((1u << hi) - 1) & ~((1u << lo) - 1), total;
     uint32_t rank = found + manager_scan((uint32_t)__builtin_popcount(mine), smem, &total);
     for (; mine; mine &= mine - 1) visit((int32_t)(p0 + __builtin_ctz(mine)), rank++);
     found += total;
@@ -144,8 +150,8 @@ __global__ __launch_bounds__(kBlock) void fork_kernel(PoolView p, const int32_t 
 }
 
 // Pages for the sessions' new positions, a thread per session: the list of tail pages to copy, and the pages taken, in order.
-// kCopies: the tails are so small that this workgroup copies them too (4 beams, pages of 32 KB: 5.4 us where two kernels took
-// 6.6 and 2.9, and a launch less for the host).
+// kCopies: the tails are so small that this workgroup copies them too, a launch less (the step of 4 beams with pages of 32 KB
+// that calls it: 19.4 against 22.2 us).
 struct CopyList {
   uint32_t count, pad[3];
   int32_t from[kManager], to[kManager], rows[kManager];
@@ -155,10 +161,12 @@ __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int3
                                                           CopyList *__restrict__ copies, int32_t *__restrict__ taken,
                                                           uint32_t *status) {
   __shared__ uint32_t smem[kManager / 64 + 1];
-  __shared__ int32_t tails[kManager], first_of[kManager];
+  __shared__ __attribute__((aligned(16))) int32_t tails[kManager];
+  __shared__ int32_t first_of[kManager];
   __shared__ uint32_t start_of[kManager];
   __shared__ uint32_t refused;
   const int32_t s = threadIdx.x;
+  const uint32_t ready = used_bits(p, (int64_t)s * kScanWords);
   if (s == 0) refused = 0;
   __syncthreads();
   int64_t len = 0, g = 0;
@@ -199,7 +207,10 @@ __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int3
   bool copy = false;
   if (held > 1) {
     int32_t before = 0;
-    for (int32_t o = 0; o < s; ++o) before += tails[o] == tail;
+    for (int32_t o = 0; o < s; o += 4) {
+      const int4 t = *reinterpret_cast<const int4 *>(tails + o);
+      before += (t.x == tail) + (o + 1 < s && t.y == tail) + (o + 2 < s && t.z == tail) + (o + 3 < s && t.w == tail);
+    }
     copy = held - before > 1;
   }
   const int32_t first = copy ? slot : pages_of(len, p.shift);
@@ -210,10 +221,9 @@ __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int3
   start_of[s] = start;
   first_of[s] = first;
   __syncthreads();
-  const uint32_t found = scan_pages(p.refs, 0, p.P, total, smem, [](int32_t r) { return r == 0; },
-                                    [&](int32_t page, uint32_t rank) {
-                                      if (rank < total) taken[rank] = page;
-                                    });
+  const uint32_t found = scan_pages(p, 0, p.P, false, ready, total, smem, [&](int32_t page, uint32_t rank) {
+    if (rank < total) taken[rank] = page;
+  });
   __syncthreads();
   if (found < total) {
     if (s == 0) {
@@ -303,14 +313,12 @@ __global__ __launch_bounds__(kManager) void compact_kernel(PoolView p, MoveList 
                                                            int32_t *__restrict__ holes, int32_t *__restrict__ movers,
                                                            int32_t *__restrict__ home, uint32_t *__restrict__ used_out) {
   __shared__ uint32_t smem[kManager / 64 + 1];
-  const uint32_t all = 0xffffffffu;
-  const auto in_use = [](int32_t r) { return r != 0; };
-  const uint32_t used = scan_pages(p.refs, 0, p.P, all, smem, in_use, [](int32_t, uint32_t) {});
+  const uint32_t all = 0xffffffffu, ready = used_bits(p, (int64_t)threadIdx.x * kScanWords);
+  const uint32_t used = scan_pages(p, 0, p.P, true, ready, all, smem, [](int32_t, uint32_t) {});
   for (int32_t page = (int32_t)used + (int32_t)threadIdx.x; page < p.P; page += kManager) home[page] = -1;
-  const uint32_t n = scan_pages(p.refs, (int32_t)used, p.P, all, smem, in_use,
+  const uint32_t n = scan_pages(p, (int32_t)used, p.P, true, ready, all, smem,
                                 [&](int32_t page, uint32_t rank) { movers[rank] = page; });
-  scan_pages(p.refs, 0, (int32_t)used, n, smem, [](int32_t r) { return r == 0; },
-             [&](int32_t page, uint32_t rank) { holes[rank] = page; });
+  scan_pages(p, 0, (int32_t)used, false, ready, n, smem, [&](int32_t page, uint32_t rank) { holes[rank] = page; });
   __syncthreads();
   for (uint32_t r = threadIdx.x; r < n; r += kManager) {
     const int32_t from = movers[r], to = holes[r];
