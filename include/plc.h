@@ -622,7 +622,8 @@ int plc_trie_evict(plc_trie *trie, int64_t id);
  *   lens     i32 [S]: positions of each session.
  *   refs     i32 [P]: number of table entries that name the page.  A page is free while it is 0.
  * The caller fills table with -1 and lens and refs with zeros once; from then on the calls below keep them.
- * All calls work in place and in stream order.  They raise status PLC_ERR_INVALID for lengths, page numbers or
+ * All calls work in place and in stream order; calls on one pool, or with one workspace, must not overlap (on two streams,
+ * the later one waits for the earlier).  They raise status PLC_ERR_INVALID for lengths, page numbers or
  * offsets that are not what is described here (the rows concerned are left alone), and never read or write
  * outside the buffers.  What they do depends on their arguments alone, not on the order in which workgroups run:
  * pages are taken from the lowest free number on.
@@ -695,13 +696,13 @@ int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *
  *   score  s_p = scale * sum_e q[e] * k_p[e] over the positions p that the node sees: all p < c, itself, and its
  *          ancestors in the tree (`parents`), or all nodes before it (parents = null: a chain);
  *   out    sum_p exp(s_p) v_p / sum_p exp(s_p),   lse = ln sum_p exp(s_p).
- * Products of 16-bit values accumulated in fp32, maximum and sum in fp32; the weights are rounded to the cache's
- * type, relative to the largest so far, for the product with v.  Rows that a node does not see have no effect on
- * it, whatever they hold.  Sessions without nodes take no part.
+ * Products of 16-bit values accumulated in fp32, maximum and sum in fp32; for the product with v the weights are rounded to
+ * the cache's type, relative to a maximum that may lag behind the largest score by 8 powers of two.  Rows that a node does
+ * not see have no effect on it, whatever they hold.  Sessions without nodes take no part.
  *   layer      0..L-1.
  *   type       PLC_FP16 or PLC_BF16, of the cache, q and out.  d <= 256.
  *   q, out     logical [N, H*G, d], element strides (node, head) in q_stride / out_stride, multiples of 8;
- *              16-byte aligned.  Node x of the call is row x.
+ *              16-byte aligned.  Node x of the call is row x; rows behind off[S] are left alone.
  *   off        as above, off[S] <= N.
  *   parents    nullable: i32 [N], the number within the tree of a node's parent, less than its own; -1: the node
  *              continues the cache.

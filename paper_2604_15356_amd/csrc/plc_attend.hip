@@ -16,11 +16,12 @@
 // cut where they are long, or where there are few rows and heads to fill the chip with (attend_plan has the rule).
 // Workgroups take the chunks in turn; what a cut has split is joined by a second kernel.
 //
-// What bounds it: few rows, HBM (64 sessions of one token, 8 heads, 4 query heads each, up to 4096 positions: 545 MB in 112 us,
-// 4.9 TB/s; a large copy reaches 4.9); many rows, the turns of the matrix cores and the vector units (64 nodes, 32,768
-// positions: 34 GFLOP in 57 us with the joining, 0.60 PFLOP/s; the matrix cores are busy a third of the time, the softmax and
-// its waits take the rest); short contexts, the 4 us from a workgroup's start to its first products (offsets, table, pages,
-// one after the other) and 3.5 us of its end.
+// What bounds it: few rows, HBM (64 sessions of one token, 8 heads, 4 query heads each, up to 4096 positions: 547 MB in
+// 111 us, 4.9 TB/s; a copy of 4 GB reaches 4.9).  Many rows, the turns of the matrix cores and the vector units (64 nodes,
+// 32,768 positions: 34 GFLOP in 58 us with the joining, 0.59 PFLOP/s; the matrix cores are busy 0.35 of the kernel's 51 us,
+// vector instructions are issued in 0.39, a third of their time the wavefronts wait at barriers and for LDS).  Short contexts,
+// the 4 us from a workgroup's start to its first products (offsets, table, pages, one after the other) and 3.5 us of its end.
+#include <atomic>
 #include <type_traits>
 
 #include "plc_device.h"
@@ -846,10 +847,15 @@ template <class T, class Shape>
 void launch_attend(const AttendArgs &a, const AttendPlan &plan, hipStream_t st) {
   const bool exact = 8 * a.p.d8 == Shape::DP;
   const auto kernel = exact ? &attend_kernel<T, Shape, true> : &attend_kernel<T, Shape, false>;
-  static const hipError_t sized[2] = {  // once: it costs a call's host time over again
-      hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, Shape, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds),
-      hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, Shape, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds)};
-  (void)sized;
+  static std::atomic<uint64_t> sized{0};  // devices that know of the kernels' LDS: to tell them costs a call's host time over again
+  int device = 0;
+  (void)hipGetDevice(&device);
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (!(sized.load(std::memory_order_relaxed) & bit)) {
+    for (const auto f : {&attend_kernel<T, Shape, false>, &attend_kernel<T, Shape, true>})
+      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Shape::kLds);
+    sized.fetch_or(bit, std::memory_order_relaxed);
+  }
   hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.line < kMostGroups ? plan.line : kMostGroups)), dim3(Shape::kThreads), Shape::kLds, st, a);
 }
 

@@ -5,7 +5,8 @@ A cache that codec.py has decoded is put to work here: `store` takes the decoder
 on from each other's prefix (what PrefixTrie.best_match found, the beams of a search), `extend` makes room for the tokens of
 a step or for a tree of drafted ones, `attend` computes their attention, `accept` keeps the verified nodes, and `load` gives
 the rows back for the encoder.  Everything works in place, in the order of the current stream, without synchronising;
-errors in the data show in `check_status`."""
+errors in the data show in `check_status`.  A cache is used from one stream at a time: its workspaces are its own.
+examples/speculative_decoding.py has all of it in a serving loop."""
 from __future__ import annotations
 
 import torch
