@@ -165,6 +165,13 @@ def test_chunks_follow_the_sessions_lengths(lens):
     check(torch.float16, 64, 2, 1, 16, lens, [1 + (i % 2) * (n > 1) for i, n in enumerate(lens)], True, seed=len(lens))
 
 
+@pytest.mark.parametrize("d", [64, 128, 200, 256])
+@pytest.mark.parametrize("G,t", [(2, 1), (5, 9), (6, 30)])
+def test_contexts_cut_in_some_parts(d, G, t):
+    """A dozen tiles and heads: parts enough for several groups of lanes to join, in every arrangement of rows."""
+    check(torch.bfloat16, d, G, 1, 32, [1500 + 97 * i for i in range(12)], [t - i % 2 * (t > 1) for i in range(12)], True, seed=d + t)
+
+
 def test_strides_layers_and_scales():
     for layer in range(3):
         check(torch.float16, 80, 2, 3, 16, [50, 7], [5, 7], True, seed=layer, layout="gaps", L=3, layer=layer, scale=0.3)

@@ -330,6 +330,31 @@ def test_data_that_cannot_be_used_is_refused():
         assert torch.equal(cache.k, before)
 
 
+@pytest.mark.parametrize("n", [3001, 4097])
+def test_rows_on_both_sides_of_what_the_caches_hold(n):
+    """As many rows as are stored through the caches, and more: every element, and nothing else, is where it belongs."""
+    L, H, B, d = 4, 8, 16, 128
+    assert (n * L * H * d * 8 > 96 << 20) == (n > 4000)
+    torch.manual_seed(n)
+    cache = make(-(-n // B) + 2, L, H, B, d, 1, -(-n // B))
+    before = cache.k.clone()
+    cache.extend(ints([n]))
+    k, v = (torch.randn((1, L, H, n, d), device=DEV, dtype=torch.float16) for _ in range(2))
+    cache.store(k, v, offsets([n]))
+    cache.check_status()
+    for pool, rows in ((cache.k, k), (cache.v, v)):
+        used = pool[cache.table[0].long()].permute(1, 2, 0, 3, 4).flatten(2, 3)  # [L, H, rows, d]
+        assert torch.equal(used[:, :, :n], rows[0])
+    rest = torch.ones(cache.P, dtype=torch.bool, device=DEV)
+    rest[cache.table[0].long()] = False
+    assert torch.equal(cache.k[rest], before[rest])
+    last = int(cache.table[0, -1])
+    assert n % B == 0 or torch.equal(cache.k[last, :, :, n % B:], before[last, :, :, n % B:])
+    out, out2 = torch.zeros_like(k), torch.zeros_like(v)
+    cache.load(out, out2, offsets([n]))
+    assert torch.equal(out, k) and torch.equal(out2, v)
+
+
 def test_pages_beyond_32_bits():
     """A pool whose halves have more than 2^31 elements: the last page is as good as the first."""
     L, H, B, d = 4, 8, 64, 128
