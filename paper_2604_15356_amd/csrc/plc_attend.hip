@@ -18,7 +18,7 @@
 //
 // What bounds it: few rows, HBM (64 sessions of one token, 8 heads, 4 query heads each, up to 4096 positions: 547 MB in
 // 111 us, 4.9 TB/s; a copy of 4 GB reaches 4.9).  Many rows, the turns of the matrix cores and the vector units (64 nodes,
-// 32,768 positions: 34 GFLOP in 58 us with the joining, 0.59 PFLOP/s; the matrix cores are busy 0.35 of the kernel's 51 us,
+// 32,768 positions: 34 GFLOP in 60 us with the joining, 0.57 PFLOP/s; the matrix cores are busy 0.35 of the kernel's 51 us,
 // vector instructions are issued in 0.39, a third of their time the wavefronts wait at barriers and for LDS).  Short contexts,
 // the 4 us from a workgroup's start to its first products (offsets, table, pages, one after the other) and 3.5 us of its end.
 #include <atomic>
@@ -536,6 +536,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[m][i] *= keep;
       }
+      // The weights, rounded to the type of V, for a matrix product of 16-bit values: half a step each, as the result is rounded
+      // once more at its end.  (In 32 bits the product would take two such products.)  Their sum takes them unrounded.
       short8v pf[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n)

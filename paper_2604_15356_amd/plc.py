@@ -644,10 +644,14 @@ def plc_attend(pages, layer, q, off, parents, max_nodes, max_len, scale, out, ls
         raise ValueError("query heads are a multiple of the cache's, with as many components")
     if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous()):
         raise TypeError("lse is contiguous float32")
-    _check(lib().plc_attend(pages, layer, PLC_FP16 if q.dtype is torch.float16 else PLC_BF16, _on_device(q), _I64x2(qs[0], qs[1]),
+    if not (q.is_cuda and out.is_cuda and ws.is_cuda and (lse is None or lse.is_cuda)):
+        raise ValueError("plc takes device tensors")
+    q_stride = _I64x2(qs[0], qs[1])
+    _check(lib().plc_attend(pages, layer, PLC_FP16 if q.dtype is torch.float16 else PLC_BF16, q.data_ptr(), q_stride,
                             shape[1] // pages.H, shape[0], _ints(off), None if parents is None else _ints(parents), max_nodes,
-                            max_len, scale, _on_device(out), _I64x2(os_[0], os_[1]), None if lse is None else _on_device(lse),
-                            _on_device(ws), ws.numel(), _ints(status), _raw_stream(q.device.index)), "plc_attend")
+                            max_len, scale, out.data_ptr(), q_stride if os_ == qs else _I64x2(os_[0], os_[1]),
+                            None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _ints(status),
+                            _raw_stream(q.get_device())), "plc_attend")
 
 
 class PrefixTrie:
