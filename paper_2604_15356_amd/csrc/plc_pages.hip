@@ -218,9 +218,20 @@ __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int3
   }
   const int32_t first = copy ? slot : pages_of(len, p.shift);
   const uint32_t need = (uint32_t)(pages_of(len + g, p.shift) - first);
-  uint32_t total, n_copies;
+  // A session may ask for 2^26 pages, all of them together for more than 32 bits count: the second sum takes the needs'
+  // multiples of 2^21 along, above the copies.  Unless those alone are more than the pool has, the first sum is below
+  // P + 1024 * 2^21 < 2^32, and exact.
+  uint32_t total, sums;
   const uint32_t start = manager_scan(need, smem, &total);
-  const uint32_t nth = manager_scan(copy ? 1u : 0u, smem, &n_copies);
+  const uint32_t nth = manager_scan((need >> 21) << 11 | (copy ? 1u : 0u), smem, &sums) & 2047u;
+  const uint32_t n_copies = sums & 2047u;
+  if ((uint64_t)(sums >> 11) << 21 > (uint64_t)p.P) {
+    if (s == 0) {
+      copies->count = 0;
+      raise(status, PLC_ERR_CAPACITY);
+    }
+    return;
+  }
   start_of[s] = start;
   first_of[s] = first;
   __syncthreads();

@@ -385,3 +385,25 @@ def test_pages_beyond_32_bits():
     cache.check_status()
     cache.load(out, out2, offsets([0, 8]))
     assert torch.equal(out2, rows2[keep]) and cache.table[:, 0].tolist() == [0, 1]
+
+
+@pytest.mark.parametrize("S", [64, 65])
+def test_more_room_than_32_bits_count(S):
+    """Tables so wide that the pages asked for in one call are 2^32 and more: refused like any other, and nothing changes."""
+    M, B = 1 << 26, 16
+    cache = make(6, 1, 1, B, 8, 1, 1)
+    table = torch.empty((S, M), dtype=torch.int32, device=DEV)  # (entries behind a session's pages are not looked at)
+    table[:2, :2] = ints([[3, -1], [3, -1]])
+    lens, refs = ints([5, 5] + [0] * (S - 2)), ints([0, 0, 0, 2, 0, 0])
+    cache = PagedKVCache(cache.k, cache.v, table, lens, refs)
+    before = [x.clone() for x in (cache.k, cache.v, table[:, :2].contiguous(), lens, refs)]
+    for grow in ([M * B - 5] * 2 + [M * B] * (S - 2), [M * B - 5] + [0] * (S - 1), [M * B - 5] * 2 + [1 << 29] * (S - 2)):
+        cache.extend(ints(grow))
+        with pytest.raises(plc.PlcError) as e:
+            cache.check_status()
+        assert e.value.code == plc.PLC_ERR_CAPACITY
+        for x, b in zip((cache.k, cache.v, table[:, :2], lens, refs), before):
+            assert torch.equal(x.contiguous().view(torch.int16), b.view(torch.int16))
+    cache.extend(ints([1, 1] + [0] * (S - 2)))  # what there is room for is still given
+    cache.check_status()
+    assert lens.tolist() == [6, 6] + [0] * (S - 2) and refs.tolist() == [1, 0, 0, 1, 0, 0] and table[:2, 0].tolist() == [0, 3]
