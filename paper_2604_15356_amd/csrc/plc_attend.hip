@@ -575,13 +575,14 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         short8v vf[2][MD];
         read_transposed<n * (32 * DP * 2), 16 * DP * 2>(v_here, vf);
         if (odd[n]) {  // a weight of zero must not meet them: they are added by hand where the weight is not zero
+          const uint32_t mine = odd[n] >> (4 * half);
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int m = 0; m < MD; ++m)
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                if (special<T>((uint16_t)vf[u][m][e])) vf[u][m][e] = 0;
+                if ((mine >> (16 * u + 8 * (e >> 2) + (e & 3)) & 1u) && special<T>((uint16_t)vf[u][m][e])) vf[u][m][e] = 0;
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)

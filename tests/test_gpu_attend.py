@@ -365,3 +365,28 @@ def test_a_cache_beyond_32_bits():
     want, want_lse, absolute, size = definition(q, *packed, lens, [3, 1], [-1, -1, 0, -1], G, d ** -0.5)
     tol, tol_lse = bounds(torch.bfloat16, d, 3 * B, want, want_lse, absolute, size, 0)
     assert bool(((got.double().cpu() - want).abs() <= tol).all()) and bool(((lse.double().cpu() - want_lse).abs() <= tol_lse).all())
+
+
+@BOTH
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("G,H,d", [(1, 1, 64), (8, 1, 64), (16, 1, 64), (2, 1, 256), (8, 1, 256), (16, 1, 256), (16, 1024, 8)])
+def test_infinite_values_where_context_and_tree_meet(dtype, bad, G, H, d):
+    """A context that ends inside a block of 32 positions, an infinity or a NaN in V of its last rows, others in the tree and
+    behind the end: what everybody sees reaches everybody, what a node does not see has no effect on it."""
+    t, n = 6, 76
+    parents = [-1, 0, 1, -1, 3, 4]
+    cache, (k, v) = make(dtype, d, H, 16, [n], seed=G + d, fill=bad)
+    q = torch.randn((t, H * G, d), device=DEV).to(dtype)
+    clean, clean_lse = cache.attend(q, offsets([t]), parents=ints(parents), max_nodes=t)
+    assert torch.isfinite(clean).all()
+    v2 = v.clone()
+    v2[n - t - 4, 0, :, 5] = bad   # in the context
+    v2[n - t + 1, 0, :, 3] = bad   # nodes 1 and 2 see it
+    cache.store(k, v2, offsets([n]))
+    got, lse = cache.attend(q, offsets([t]), parents=ints(parents), max_nodes=t)
+    cache.check_status()
+    touched = torch.zeros((t, H * G, d), dtype=torch.bool, device=DEV)
+    touched[..., 5] = True
+    touched[1:3, :, 3] = True
+    is_bad = torch.isnan(got) if bad != bad else got == bad
+    assert is_bad[touched].all() and torch.equal(got[~touched], clean[~touched]) and torch.equal(lse, clean_lse)
