@@ -390,3 +390,94 @@ def test_infinite_values_where_context_and_tree_meet(dtype, bad, G, H, d):
     touched[1:3, :, 3] = True
     is_bad = torch.isnan(got) if bad != bad else got == bad
     assert is_bad[touched].all() and torch.equal(got[~touched], clean[~touched]) and torch.equal(lse, clean_lse)
+
+
+def definition_by_heads(q, k, v, lens, counts, parents, G, scale):
+    """What `definition` gives, a session at a time with all of its heads, on the device."""
+    N, heads, d = q.shape
+    H = heads // G
+    out, absolute = (torch.zeros((N, heads, d), dtype=torch.float64, device=DEV) for _ in range(2))
+    lse, size = (torch.zeros((N, heads), dtype=torch.float64, device=DEV) for _ in range(2))
+    row0 = x = 0
+    for n, t in zip(lens, counts):
+        if t:
+            sees = torch.zeros((t, n), dtype=torch.bool)
+            sees[:, : n - t] = True
+            for i in range(t):
+                a = i
+                while a >= 0:
+                    sees[i, n - t + a] = True
+                    a = parents[x + a] if parents is not None else a - 1
+            hidden = ~sees.to(DEV).repeat_interleave(G, 0)  # [t G, n]
+            qs = q[x: x + t].double().view(t, H, G, d).transpose(0, 1).reshape(H, t * G, d)
+            ks, vs = (r[row0: row0 + n].double().transpose(0, 1).contiguous() for r in (k, v))
+            turned = ks.transpose(1, 2).contiguous()
+            s = (scale * (qs @ turned)).masked_fill(hidden, -math.inf)
+            w = torch.softmax(s, 2)
+            back = lambda y: y.view(H, t, G, -1).transpose(0, 1).reshape(t, heads, -1)  # noqa: E731
+            out[x: x + t], absolute[x: x + t] = back(w @ vs), back(w @ vs.abs())
+            lse[x: x + t] = back(torch.logsumexp(s, 2, keepdim=True))[..., 0]
+            size[x: x + t] = back((scale * (qs.abs() @ turned.abs())).masked_fill(hidden, 0).amax(2, keepdim=True))[..., 0]
+        x += t
+        row0 += n
+    return out.cpu(), lse.cpu(), absolute.cpu(), size.cpu()
+
+
+def check_by_heads(dtype, d, G, H, B, lens, counts, tree, seed, **kw):
+    """`check` for many heads and long contexts."""
+    rng = random.Random(seed)
+    cache, (k, v) = make(dtype, d, H, B, lens, seed)
+    q = torch.randn((sum(counts), H * G, d), device=DEV).to(dtype)
+    parents = [p for t in counts for p in random_tree(rng, t)] if tree else None
+    got, lse = cache.attend(q, offsets(counts), parents=None if parents is None else ints(parents), max_nodes=max(counts),
+                            max_len=max(lens), **kw)
+    cache.check_status()
+    want, want_lse, absolute, size = definition_by_heads(q, k[:, 0], v[:, 0], lens, counts, parents, G, d ** -0.5)
+    tol, tol_lse = bounds(dtype, d, max(lens), want, want_lse, absolute, size, float(v.abs().max()))
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
+    off = (lse.double().cpu() - want_lse).abs()
+    assert bool((off <= tol_lse).all()), float((off / tol_lse).max())
+
+
+@BOTH
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("d", [64, 96, 128, 200])
+@pytest.mark.parametrize("G,t", [(2, 3), (20, 2), (9, 9), (7, 23)])
+def test_workgroups_that_take_several_chunks(dtype, tree, d, G, t):
+    """2560 tiles and heads and more, of which 2048 workgroups take one or several: what one chunk has left in the shared
+    memory is not what the next one reads."""
+    lens = [t + (13 * i) % 90 for i in range(40)]
+    check_by_heads(dtype, d, G, 64, 16, lens, [t - (i % 3) * (t > 3) for i in range(40)], tree, seed=d + G)
+
+
+@BOTH
+@pytest.mark.parametrize("d", [64, 128, 200])
+@pytest.mark.parametrize("S,H,longest", [(8, 32, 9000), (8, 64, 9000), (4, 64, 25000), (20, 64, 9000)])
+@pytest.mark.parametrize("G,t", [(2, 1), (20, 2), (4, 23)])
+def test_many_tiles_and_heads_of_long_contexts(dtype, d, S, H, longest, G, t):
+    """As many tiles and heads as there are compute units, or more, and a context that is cut all the same: partial results
+    of every arrangement of rows, of short sessions beside them, and of workgroups that take several chunks."""
+    lens = [t + (37 * i) % 200 for i in range(S)]
+    lens[S // 2] = longest
+    check_by_heads(dtype, d, G, H, 16, lens, [t] * S, True, seed=d + S)
+
+
+@BOTH
+@pytest.mark.parametrize("d,B", [(64, 64), (96, 16), (256, 32)])
+@pytest.mark.parametrize("t,n", [(130, 130), (257, 700), (600, 2500)])
+def test_chains_of_many_nodes(dtype, d, B, t, n):
+    """A prompt's pieces in other types, widths and pages than `test_chains_of_a_prompts_pieces`."""
+    check_by_heads(dtype, d, 3, 2, B, [n, 77], [t, 40], False, seed=t)
+
+
+def test_the_same_call_gives_the_same():
+    """Parts are joined in a fixed order: a call repeats itself bit for bit."""
+    for lens, t, G in (([5000, 20011, 700], 9, 4), ([3000], 1, 4), ([4000, 90, 1200, 40], 40, 3)):
+        cache, _ = make(torch.bfloat16, 128, 2, 16, lens, seed=t)
+        q = torch.randn((t * len(lens), 2 * G, 128), device=DEV).to(torch.bfloat16)
+        first = cache.attend(q, offsets([t] * len(lens)), max_nodes=t)
+        for _ in range(5):
+            again = cache.attend(q, offsets([t] * len(lens)), max_nodes=t)
+            assert all(torch.equal(a, b) for a, b in zip(first, again))
+        cache.check_status()
