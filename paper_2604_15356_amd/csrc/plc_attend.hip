@@ -528,7 +528,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       const Halves both = halves(most);
       most = fmaxf(both.lo, both.hi) * a.scale2;
       if (__ballot(most > top + kSlack) != 0) {
-        const float now = fmaxf(top, most), keep = __builtin_amdgcn_exp2f(top - now);
+        const float now = most > top + kSlack ? most : top;  // (by a row's own scores: the others must not show in its roundings)
+        const float keep = __builtin_amdgcn_exp2f(top - now);
         top = now;
         sum *= keep;
 #pragma unroll

@@ -481,3 +481,19 @@ def test_the_same_call_gives_the_same():
             again = cache.attend(q, offsets([t] * len(lens)), max_nodes=t)
             assert all(torch.equal(a, b) for a, b in zip(first, again))
         cache.check_status()
+
+
+@BOTH
+@pytest.mark.parametrize("d,G,t,n", [(64, 4, 5, 600), (128, 8, 5, 3000), (128, 8, 30, 900), (256, 8, 4, 500)])
+def test_a_rows_result_is_its_own(dtype, d, G, t, n):
+    """Other rows of a tile with larger scores, whose maxima move in other places, do not show in a row's result."""
+    cache, _ = make(dtype, d, 1, 16, [n], seed=t)
+    q = torch.randn((t, G, d), device=DEV).to(dtype)
+    parents = ints(random_tree(random.Random(t), t))
+    first, first_lse = cache.attend(q, offsets([t]), parents=parents, max_nodes=t)
+    for factor in (4.0, 30.0):
+        other = q.clone()
+        other[:, 1:] *= factor
+        got, lse = cache.attend(other, offsets([t]), parents=parents, max_nodes=t)
+        assert torch.equal(got[:, 0], first[:, 0]) and torch.equal(lse[:, 0], first_lse[:, 0])
+    cache.check_status()
