@@ -696,7 +696,7 @@ int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *
  *   score  s_p = scale * sum_e q[e] * k_p[e] over the positions p that the node sees: all p < c, itself, and its
  *          ancestors in the tree (`parents`), or all nodes before it (parents = null: a chain);
  *   out    sum_p exp(s_p) v_p / sum_p exp(s_p),   lse = ln sum_p exp(s_p).
- * Products of 16-bit values accumulated in fp32, maximum and sum in fp32; for the product with v the weights are rounded to
+ * Products of 16-bit values accumulated in fp32, maximum and sum in fp32 (scores of magnitudes up to 2^127 / log2(e)); for the product with v the weights are rounded to
  * the cache's type, relative to a maximum that may lag behind the largest score by 8 powers of two.  Rows that a node does
  * not see have no effect on it, whatever they hold.  Sessions without nodes take no part.
  *   layer      0..L-1.

@@ -38,7 +38,8 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef const __attribute__((address_space(4))) int32_t const_int;  // read through the scalar cache: not written meanwhile
 
-constexpr float kLowest = -1.0e30f;   // stands for "nothing seen yet" in the running maximum (base-2 logarithms)
+constexpr float kLowest = -__FLT_MAX__;  // stands for "nothing seen yet" in the running maximum (base-2 logarithms)
+constexpr float kFar = 0x1p20f;       // maxima from which on scores are rounded before the maximum is subtracted
 constexpr float kSlack = 8.0f;        // the maximum that weights are relative to may lag by so much: 2^8 in a weight
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 constexpr int kMaskWords = PLC_TREE_NODES / 64;
@@ -183,8 +184,7 @@ struct AttendShape {
   static constexpr size_t kMeet = PG > 1 ? (size_t)PG * kRows * (kOutRow + 2) * 4 : 0;
   static constexpr size_t kStages = (size_t)PG * kBuffers * kStage;
   static constexpr size_t kMain = kStages > kMeet ? kStages : kMeet;
-  static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4 + kLineWords * 4;
-  
+  static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4 + kLineWords * 4 + 2 * 4;
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   static constexpr int kWavesPerSimd = DP <= 128 ? 2 : 1;
 };
@@ -271,6 +271,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   const int lane_id = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rg = wave % RG, pg = wave / RG;
   uint32_t *const line = reinterpret_cast<uint32_t *>(up + PLC_TREE_NODES);
+  uint32_t *const raised = line + kLineWords;  // by a wavefront: the number of its chunk, in turn in two places
   Line mine;
   {
     bool bad = false;
@@ -283,7 +284,9 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   const uint32_t total = scalar(mine.total), chunk = scalar(mine.chunk);
   bool bad_page = false;
 
-  for (uint32_t at = blockIdx.x; at < total; at += gridDim.x) {
+  int turns = 0;
+  bool again = false;  // the chunk is gone through a second time, with what few rows need and all would wait for
+  for (uint32_t at = blockIdx.x; at < total; at += again ? 0 : gridDim.x, turns ^= 1) {
   // (what follows from the lane is worked out again for every chunk, and again behind its positions: kept in registers
   // throughout it would not leave room for two wavefronts a SIMD)
   int lane = lane_id;
@@ -537,6 +540,16 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[m][i] *= keep;
       }
+      // A fused product less the maximum keeps what the maximum's own rounding has lost: a common factor of a row's weights, next
+      // to one up to kFar (2^(2^-4)), and without bounds beyond it.
+      float by = a.scale2;
+      if (again && fabsf(top) > kFar) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[n][i] *= a.scale2;
+        by = 1.0f;
+      }
       // The weights, rounded to the type of V, for a matrix product of 16-bit values: half a step each, as the result is rounded
       // once more at its end.  (In 32 bits the product would take two such products.)  Their sum takes them unrounded.
       short8v pf[NT][2];
@@ -544,7 +557,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], a.scale2, -top));
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], by, -top));
           sum += w;
           sc[n][i] = w;
           pf[n][i >> 3][i & 7] = (short)round16<T>(w);
@@ -619,6 +632,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     }
   }
   {
+    const bool wants = fabsf(top) > kFar && top != kLowest;
+    if (!again && __ballot(wants) != 0 && lane == 0) raised[turns] = ~at;
+    __syncthreads();  // everybody is done with the stages and the masks
+    // (A word that is there by chance costs time, and nothing else.  Nobody writes in this place again before everybody has
+    // come to the barrier of the next turn, and so has read it.)
+    again = !again && raised[turns] == ~at;
+    if (again) continue;
+  }
+  {
     const Halves both = halves(sum);
     sum = both.lo + both.hi;
   }
@@ -661,12 +683,10 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         }
       }
     }
-    __syncthreads();  // (the masks are free)
     continue;
   }
 
   // the positions groups meet: their sums, relative to the largest maximum, row by row
-  __syncthreads();
   float *const meet = reinterpret_cast<float *>(attend_lds);            // [PG][kRows][kOutRow]
   float *const meet_ml = meet + PG * Shape::kRows * Shape::kOutRow;     // [PG][kRows][2]
   {

@@ -497,3 +497,38 @@ def test_a_rows_result_is_its_own(dtype, d, G, t, n):
         got, lse = cache.attend(other, offsets([t]), parents=parents, max_nodes=t)
         assert torch.equal(got[:, 0], first[:, 0]) and torch.equal(lse[:, 0], first_lse[:, 0])
     cache.check_status()
+
+
+@pytest.mark.parametrize("exponent", [11, 20, 40, 50, 58])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("d,G,n", [(64, 1, 40), (64, 40, 700), (128, 2, 9000), (256, 3, 300)])
+def test_scores_of_any_size(d, G, n, sign, exponent):
+    """Scores all over the range of fp32, to both sides: equal ones share their weight, those of twice the size have none or
+    all of it.  (Powers of two: every product and sum is exact, so that equal scores are equal.)"""
+    cache, (k, v) = make(torch.bfloat16, d, 1, 16, [n], seed=8)
+    big = torch.arange(n) % 7 < 3
+    size = torch.where(big, 2.0, 1.0) * 2.0 ** exponent
+    cache.store(size.to(DEV).to(torch.bfloat16)[:, None, None, None].expand_as(k).contiguous(), v, offsets([n]))
+    q = torch.full((1, G, d), sign * 2.0 ** exponent, dtype=torch.bfloat16, device=DEV)
+    got, lse = cache.attend(q, offsets([1]))
+    cache.check_status()
+    kept = big if sign > 0 else ~big
+    score = sign * (2.0 if sign > 0 else 1.0) * 4.0 ** exponent * d ** 0.5
+    count = int(kept.sum())
+    want, absolute = v[:, 0, 0].double().cpu()[kept].mean(0), v[:, 0, 0].double().cpu()[kept].abs().mean(0)
+    # the weights' rounding and the result's, each half a step of bf16, and sums in 32 bits
+    tol = (2.0 ** -8 * 1.01 + 4 * (n + 4) * 2.0 ** -24) * absolute + 2.0 ** -8 * 1.01 * want.abs()
+    assert bool(((got[0].double().cpu() - want).abs() <= tol).all())
+    assert bool(((lse.double().cpu() - (score + math.log(count))).abs() <= abs(score) * 4 * 2.0 ** -24 + (n + 4) * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("G,t,n", [(4, 5, 600), (8, 30, 900), (4, 2, 9000)])
+def test_far_scores_of_other_rows_do_not_show(G, t, n):
+    cache, _ = make(torch.bfloat16, 128, 2, 16, [n], seed=t)
+    q = torch.randn((t, 2 * G, 128), device=DEV).to(torch.bfloat16)
+    first, first_lse = cache.attend(q, offsets([t]), max_nodes=t)
+    other = q.clone()
+    other[:, 1::2] *= 2.0 ** 30
+    got, lse = cache.attend(other, offsets([t]), max_nodes=t)
+    cache.check_status()
+    assert torch.equal(got[:, ::2], first[:, ::2]) and torch.equal(lse[:, ::2], first_lse[:, ::2])
