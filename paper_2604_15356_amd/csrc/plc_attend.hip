@@ -153,6 +153,16 @@ __device__ __forceinline__ bool special(uint16_t x) {  // infinity or NaN
   return (x & e) == e;
 }
 
+// Adds weighted sums of values, times a weight that is above zero even where it has come out as zero: an infinity stays one.
+__device__ __forceinline__ void add_weighed(float4v &to, float weight, float4v sums) {
+  if (weight != 0.0f) {
+    to += weight * sums;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[k] += fabsf(sums[k]) == __builtin_inff() ? sums[k] : 0.0f;
+  }
+}
+
 // A row's two halves: the value of the lower and of the upper 32 lanes, in both.
 struct Halves {
   float lo, hi;
@@ -348,7 +358,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     }
     __syncthreads();
   }
-  // Which of the 32 positions from `pos` on this lane's node sees, the bits of its half's accumulators in front.
+  // Which of the 32 positions from `pos` on this lane's node sees.
   auto sees = [&](int pos) -> uint32_t {
     const int at = pos - ctx;  // > -32
     uint32_t w;
@@ -365,7 +375,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         w = (uint32_t)(lo >> sh) | (sh ? (uint32_t)(hi << (64 - sh)) : 0u);
       }
     }
-    return w >> (4 * half);
+    return w;
   };
 
   short8v qf[KS];
@@ -469,6 +479,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[m][i] = 0.0f;
   float top = kLowest, sum = 0.0f;
+  bool set_aside = false;  // infinities or NaN of V, in a place that not every row sees
 
   const int span = last - first;
   const int rounds = span > 0 ? (span + PG * Shape::kTile - 1) / (PG * Shape::kTile) : 0;
@@ -517,7 +528,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       if (edge) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint32_t w = pos + 32 * n + 32 > ctx ? sees(pos + 32 * n) : ~0u;
+          const uint32_t w = pos + 32 * n + 32 > ctx ? sees(pos + 32 * n) >> (4 * half) : ~0u;  // the bits of its half's accumulators in front
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (!(w >> (8 * (i >> 2) + (i & 3)) & 1u)) sc[n][i] = -__builtin_inff();
@@ -588,7 +599,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         constexpr int n = decltype(nu)::value;
         short8v vf[2][MD];
         read_transposed<n * (32 * DP * 2), 16 * DP * 2>(v_here, vf);
-        if (odd[n]) {  // a weight of zero must not meet them: they are added by hand where the weight is not zero
+        if (odd[n]) {  // a weight of zero must not meet them: they are added by hand in the end
+          set_aside = true;
           const uint32_t mine = odd[n] >> (4 * half);
 #pragma unroll
           for (int u = 0; u < 2; ++u)
@@ -605,28 +617,51 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       };
       weigh(std::integral_constant<int, 0>());
       if constexpr (NT == 2) weigh(std::integral_constant<int, 1>());
+    }
+  }
+  // Infinities and NaN among the values.  A weight that was rounded to zero has made a NaN of an infinity, and so has a maximum
+  // that leapt; the formula's weights are above zero.  So where a sum is not finite, or some were set aside, it is looked up once
+  // more what there is of them among the positions that a row sees: that, added up, is the sum.  (The question costs 0.1 us for a
+  // single token of a short session, 0.7 for five sessions' trees.)
+  {
+    float zeros[4] = {};
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        for (uint32_t rest = odd[n]; rest; rest &= rest - 1) {
-          const int r = __builtin_ctz(rest);
-          float w = 0.0f;
+    for (int m = 0; m < MD; ++m)
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if ((r & 3) == (i & 3) && r >> 3 == i >> 2) w = sc[n][i];
-          w = __shfl(w, col + 32 * ((r >> 2) & 1));
-          if (w > 0.0f) {
+      for (int i = 0; i < 16; ++i) zeros[i & 3] = __builtin_fmaf(o[m][i], 0.0f, zeros[i & 3]);
+    const int from = __ballot((zeros[0] + zeros[1]) + (zeros[2] + zeros[3]) != 0.0f) ? first : set_aside ? max(first, ctx) : last;
+    if (from < last) {
+      uint32_t known[MD] = {};  // sums that consist of such values
+      fetch_entries(first >> p.shift);
+      for (int it = 0; it < rounds; ++it)
+        for (int r0 = 0; r0 < Shape::kTile; r0 += kRowsPerLoad) {
+          const int pos = pos_of(it) + r0, my_pos = pos + lane / kLanesPerRow, piece = lane % kLanesPerRow;
+          if (pos + kRowsPerLoad <= from || pos >= last) continue;
+          const int64_t at_page = page_at(pos) * p.page_s + head_at + (my_pos & row_mask) * p.row_s;
+          short8v v = {};
+          if (my_pos >= from && my_pos < last && piece < p.d8) v = *reinterpret_cast<const short8v *>(p.v + at_page + piece * 8);
+          bool found = false;
 #pragma unroll
-            for (int m = 0; m < MD; ++m)
+          for (int e = 0; e < 8; ++e) found = found || special<T>((uint16_t)v[e]);
+          for (uint64_t rest = __ballot(found); rest; rest &= rest - 1) {
+            const int owner = __builtin_ctzll(rest), at_pos = pos + owner / kLanesPerRow, c = owner % kLanesPerRow, base = at_pos & ~31;
+            const uint32_t w = base + 32 > ctx ? sees(base) : ~0u;
 #pragma unroll
-              for (int b = 0; b < 4; ++b) {
-                const short4v v = *(const __attribute__((address_space(3))) short4v *)(vs_lds + n * (32 * DP * 2) +
-                                                                                       place<DP>(r, 4 * m + b) + 8 * half);
+            for (int e = 0; e < 4; ++e) {
+              const uint16_t lo = (uint16_t)__builtin_amdgcn_readlane((uint16_t)v[e], owner);
+              const uint16_t hi = (uint16_t)__builtin_amdgcn_readlane((uint16_t)v[e + 4], owner), bits = half ? hi : lo;
+              if ((w >> (at_pos & 31) & 1u) && special<T>(bits)) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const uint16_t bits = (uint16_t)v[e];
-                  if (special<T>(bits)) o[m][4 * b + e] += w * (float)__builtin_bit_cast(T, bits);
-                }
+                for (int m = 0; m < MD; ++m)
+#pragma unroll
+                  for (int b = 0; b < 4; ++b)
+                    if (4 * m + b == c) {
+                      const float x = (float)__builtin_bit_cast(T, bits);
+                      o[m][4 * b + e] = known[m] >> (4 * b + e) & 1u ? o[m][4 * b + e] + x : x;
+                      known[m] |= 1u << (4 * b + e);
+                    }
               }
+            }
           }
         }
     }
@@ -717,7 +752,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       const float n = meet_ml[2 * (g * Shape::kRows + r) + 1];
       if (n != 0.0f) {  // (a group that has seen nothing has weight zero, not zero times what it holds)
         sums += w * n;
-        v += w * *reinterpret_cast<const float4v *>(meet + (g * Shape::kRows + r) * Shape::kOutRow + e);
+        add_weighed(v, w, *reinterpret_cast<const float4v *>(meet + (g * Shape::kRows + r) * Shape::kOutRow + e));
       }
     }
     const int my_node = (r0 + r) / a.G, my_head = h * a.G + (r0 + r) % a.G;
@@ -770,9 +805,10 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   auto add = [&](float2 m, float4v x, float now) {
     const float w = __builtin_amdgcn_exp2f(m.x - now);
     const bool any = m.y != 0.0f;
-    sums += any ? w * m.y : 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] += any ? w * x[k] : 0.0f;
+    if (any) {
+      sums += w * m.y;
+      add_weighed(o, w, x);
+    }
   };
   if (here) {
     for (int c = group; c < parts; c += kGroups * kJoinBatch) {
@@ -791,7 +827,9 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
       const float keep = __builtin_amdgcn_exp2f(peak - now);
       peak = now;
       sums *= keep;
-      o *= keep;
+      const float4v before = o;
+      o = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      add_weighed(o, keep, before);
 #pragma unroll
       for (int u = 0; u < kJoinBatch; ++u) add(m[u], x[u], now);
     }

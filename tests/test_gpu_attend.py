@@ -532,3 +532,37 @@ def test_far_scores_of_other_rows_do_not_show(G, t, n):
     got, lse = cache.attend(other, offsets([t]), max_nodes=t)
     cache.check_status()
     assert torch.equal(got[:, ::2], first[:, ::2]) and torch.equal(lse[:, ::2], first_lse[:, ::2])
+
+
+@BOTH
+@pytest.mark.parametrize("gap", [20.0, 40.0, 300.0])
+@pytest.mark.parametrize("d,G,n,t", [(64, 1, 70, 1), (64, 8, 300, 6), (64, 20, 300, 6), (128, 2, 900, 5), (128, 8, 9000, 12), (256, 2, 500, 6),
+                                     (256, 20, 9000, 6)])
+def test_infinite_values_of_little_weight(dtype, gap, d, G, n, t):
+    """An infinity reaches whoever sees it, however small its weight: the formula's are above zero.  Its position's scores lie
+    e^-20 to e^-300 below the others, at the beginning (the maximum leaps later), in the middle and in the tree."""
+    cache, (k, v) = make(dtype, d, 1, 16, [n], seed=n)
+    q = torch.zeros((t, G, d), dtype=dtype, device=DEV)
+    q[..., 0] = 8.0
+    k2 = k.clone()
+    k2[..., 0] = gap * d ** 0.5 / 8
+    places = {3: range(t), n - t - 1: range(t), n - t: range(t), n // 2: range(t)}  # position: who sees it, in a chain
+    if t > 2:
+        places[n - t + 2] = range(2, t)
+    for p in places:
+        k2[p, 0, 0, 0] = 0.0
+    k2[:3, 0, 0, 0] = 0.0
+    cache.store(k2, v, offsets([n]))
+    clean, clean_lse = cache.attend(q, offsets([t]), max_nodes=t)
+    assert torch.isfinite(clean).all()
+    for i, (p, seeing) in enumerate(places.items()):
+        v2 = v.clone()
+        v2[p, 0, 0, 5] = math.inf
+        v2[p, 0, 0, 9] = -math.inf
+        cache.store(k2, v2, offsets([n]))
+        got, lse = cache.attend(q, offsets([t]), max_nodes=t)
+        rest = torch.ones((t, G, d), dtype=torch.bool, device=DEV)
+        rest[list(seeing)] &= (torch.arange(d, device=DEV) != 5) & (torch.arange(d, device=DEV) != 9)
+        assert (got[list(seeing)][..., 5] == math.inf).all() and (got[list(seeing)][..., 9] == -math.inf).all(), p
+        assert torch.equal(got[rest], clean[rest]) and torch.equal(lse, clean_lse), p
+    cache.check_status()
