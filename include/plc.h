@@ -697,7 +697,8 @@ int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *
  *          ancestors in the tree (`parents`), or all nodes before it (parents = null: a chain);
  *   out    sum_p exp(s_p) v_p / sum_p exp(s_p),   lse = ln sum_p exp(s_p).
  * Products of 16-bit values accumulated in fp32, maximum and sum in fp32 (scores of magnitudes up to 2^127 / log2(e)); for the product with v the weights are rounded to
- * the cache's type, relative to a maximum that may lag behind the largest score by 8 powers of two.  Rows that a node does
+ * the cache's type, relative to a maximum that may lag behind the largest score by 8 powers of two (in fp16 7 further: weights
+ * down to 2^-21 of the largest keep all of the type's bits).  Rows that a node does
  * not see have no effect on it, whatever they hold; an infinity or a NaN in v reaches whoever sees it, however small its weight.  Sessions without nodes take no part.
  *   layer      0..L-1.
  *   type       PLC_FP16 or PLC_BF16, of the cache, q and out.  d <= 256.

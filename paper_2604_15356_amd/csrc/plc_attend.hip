@@ -273,6 +273,9 @@ template <class T, class Shape, bool kExact>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_kernel(AttendArgs a) {
   constexpr int DP = Shape::DP, RG = Shape::RG, PG = Shape::PG, NT = Shape::NT;
   constexpr int KS = DP / 16, MD = DP / 32;
+  // What weights are relative to lies this far below the maximum it was taken from: fp16 holds weights from 2^-14 on with all of
+  // its bits, down from 2^7 that is 2^-21 of the largest, and the largest, 2^7 2^8, in its range.
+  constexpr float kLift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
   extern __shared__ __attribute__((aligned(1024))) char attend_lds[];
   lds_char *const lds = (lds_char *)attend_lds;
   uint64_t *const masks = reinterpret_cast<uint64_t *>(attend_lds + Shape::kMain);  // [kRows][kMaskWords]
@@ -541,8 +544,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         for (int i = 0; i < 16; ++i) most = fmaxf(most, sc[n][i]);
       const Halves both = halves(most);
       most = fmaxf(both.lo, both.hi) * a.scale2;
-      if (__ballot(most > top + kSlack) != 0) {
-        const float now = most > top + kSlack ? most : top;  // (by a row's own scores: the others must not show in its roundings)
+      if (__ballot(most > top + (kSlack + kLift)) != 0) {
+        const float now = most > top + (kSlack + kLift) ? most - kLift : top;  // (by a row's own scores: the others must not show in its roundings)
         const float keep = __builtin_amdgcn_exp2f(top - now);
         top = now;
         sum *= keep;
@@ -562,17 +565,19 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         by = 1.0f;
       }
       // The weights, rounded to the type of V, for a matrix product of 16-bit values: half a step each, as the result is rounded
-      // once more at its end.  (In 32 bits the product would take two such products.)  Their sum takes them unrounded.
+      // once more at its end.  (In 32 bits the product would take two such products.)  Their sum takes them unrounded, a stage's
+      // by themselves first: many small ones would lose their last bits to a large sum one by one.
       short8v pf[NT][2];
+      float part_sum = 0.0f;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], by, -top));
-          sum += w;
-          sc[n][i] = w;
+          part_sum += w;
           pf[n][i >> 3][i & 7] = (short)round16<T>(w);
         }
+      sum += part_sum;
       uint32_t odd[NT];  // positions of the tree, or behind the end, that hold an infinity or a NaN
 #pragma unroll
       for (int n = 0; n < NT; ++n) odd[n] = 0;

@@ -566,3 +566,29 @@ def test_infinite_values_of_little_weight(dtype, gap, d, G, n, t):
         assert (got[list(seeing)][..., 5] == math.inf).all() and (got[list(seeing)][..., 9] == -math.inf).all(), p
         assert torch.equal(got[rest], clean[rest]) and torch.equal(lse, clean_lse), p
     cache.check_status()
+
+
+@BOTH
+def test_many_small_weights_beside_a_large_one(dtype):
+    """A first position that most of the weight goes to, and 130,000 others in one piece with the same small weight each
+    (2^-20 of the first, between two of fp16's smallest numbers): together an eighth of the sum."""
+    n, t, H, d, gap = 131072, 2048, 64, 8, 13.8125 if dtype == torch.bfloat16 else 13.8359375
+    cache, (k, v) = make(dtype, d, H, 1024, [n + t], seed=1)
+    k.zero_()
+    k[0, ..., 0] = gap
+    v.fill_(1.0)
+    v[0] = 0.0
+    cache.store(k, v, offsets([n + t]))
+    q = torch.zeros((t, H, d), dtype=dtype, device=DEV)
+    q[..., 0] = 1.0
+    got, lse = cache.attend(q, offsets([t]), scale=1.0, max_nodes=t, max_len=n + t)
+    cache.check_status()
+    small = torch.arange(n, n + t, dtype=torch.float64) * math.exp(-gap)  # those that a node sees, less the first
+    want = (small / (1 + small))[:, None, None]
+    # half a step of the type, of a weight and of the result; fp16's smallest steps next to a largest weight of 2^7; sums in 32
+    # bits, to which 16 products at a time and 32 weights are added
+    half, u = torch.finfo(dtype).eps / 2, 2.0 ** -24
+    tol = (2.02 * half + 2 * (n + t) / 16 * u + (n + t) / 32 * u) * want + (n + t) * 2.0 ** -32
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
+    assert bool(((lse.double().cpu() - (gap + (1 + small).log())[:, None]).abs() <= ((n + t) / 32 + 64) * u).all())
