@@ -707,6 +707,8 @@ int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *
  *   off        as above, off[S] <= N.
  *   parents    nullable: i32 [N], the number within the tree of a node's parent, less than its own; -1: the node
  *              continues the cache.
+ *              Where one is not that, or a page that is read is none, PLC_ERR_INVALID is raised and the rows (of out
+ *              and lse) of the session that read it are left alone.
  *   max_nodes, max_len   host: no session has more nodes, none more positions (else status PLC_ERR_INVALID is
  *              raised and the session's rows are left alone).  They set the launch: close bounds are best.  With
  *              `parents` max_nodes <= PLC_TREE_NODES.

@@ -194,7 +194,7 @@ struct AttendShape {
   static constexpr size_t kMeet = PG > 1 ? (size_t)PG * kRows * (kOutRow + 2) * 4 : 0;
   static constexpr size_t kStages = (size_t)PG * kBuffers * kStage;
   static constexpr size_t kMain = kStages > kMeet ? kStages : kMeet;
-  static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4 + kLineWords * 4 + 2 * 4;
+  static constexpr size_t kLds = kMain + (size_t)kRows * kMaskWords * 8 + PLC_TREE_NODES * 4 + kLineWords * 4 + 2 * RG * PG * 4;
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   static constexpr int kWavesPerSimd = DP <= 128 ? 2 : 1;
 };
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   const int lane_id = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rg = wave % RG, pg = wave / RG;
   uint32_t *const line = reinterpret_cast<uint32_t *>(up + PLC_TREE_NODES);
-  uint32_t *const raised = line + kLineWords;  // by a wavefront: the number of its chunk, in turn in two places
+  uint32_t *const said = line + kLineWords;  // [2][wavefronts]: what each found in its chunk, in turn in two places
   Line mine;
   {
     bool bad = false;
@@ -296,6 +296,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   const auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
   const uint32_t total = scalar(mine.total), chunk = scalar(mine.chunk);
   bool bad_page = false;
+  constexpr uint32_t kAgain = 1, kBroken = 2;
 
   int turns = 0;
   bool again = false;  // the chunk is gone through a second time, with what few rows need and all would wait for
@@ -337,12 +338,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   int node = (live ? row : R - 1) / a.G, head = h * a.G + (live ? row : R - 1) % a.G;
   const int node0 = r0 / a.G;  // of the tile
 
+  bool broken = false;  // a page or a parent is none: the chunk's rows are left alone
+
   // ancestors of the tile's nodes, where the chunk reaches into the tree
   if (!chain && last > ctx) {
     for (int i = threadIdx.x; i < t; i += Shape::kThreads) {
       int u = a.parents[n0 + i];
       if (u < -1 || u >= i) {
         raise(a.status, PLC_ERR_INVALID);
+        broken = true;
         u = -1;
       }
       up[i] = u;
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
     const int slot = min(pos >> p.shift, last_slot);
     if (slot >= slot0 + 64) fetch_entries(slot);
     const int32_t page = __builtin_amdgcn_readlane(entries, slot - slot0);
-    if (!p.page_ok(page)) bad_page = true;
+    if (!p.page_ok(page)) broken = bad_page = true;
     return p.page_ok(page) ? page : 0;
   };
   auto request = [&](int pos, int buf) {
@@ -673,12 +677,18 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
   }
   {
     const bool wants = fabsf(top) > kFar && top != kLowest;
-    if (!again && __ballot(wants) != 0 && lane == 0) raised[turns] = ~at;
+    const uint32_t mine = (!again && __ballot(wants) ? kAgain : 0) | (__ballot(broken) ? kBroken : 0);
+    if (lane == 0) said[turns * (RG * PG) + wave] = mine;
     __syncthreads();  // everybody is done with the stages and the masks
-    // (A word that is there by chance costs time, and nothing else.  Nobody writes in this place again before everybody has
-    // come to the barrier of the next turn, and so has read it.)
-    again = !again && raised[turns] == ~at;
+    // (Nobody writes in this place again before everybody has come to the barrier of the next turn, and so has read it.)
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < RG * PG; ++w) all |= said[turns * (RG * PG) + w];
+    all = scalar(all);
+    again = all & kAgain;
     if (again) continue;
+    broken = all & kBroken;
+    if (whole && broken) continue;
   }
   {
     const Halves both = halves(sum);
@@ -718,7 +728,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
         if (whole) {
           if (a.lse) a.lse[out_row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
         } else {
-          part_ml[0] = top;
+          part_ml[0] = broken ? __builtin_nanf("") : top;
           part_ml[1] = sum;
         }
       }
@@ -771,7 +781,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesPerSimd) void attend_
       const int64_t mine = (int64_t)at * Shape::kRows + r;
       *reinterpret_cast<float4v *>(a.part_o + mine * (8 * p.d8) + e) = v;
       if (e == 0) {
-        a.part_ml[2 * mine] = peak;
+        a.part_ml[2 * mine] = broken ? __builtin_nanf("") : peak;
         a.part_ml[2 * mine + 1] = sums;
       }
     }
@@ -805,6 +815,7 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
   const int r = i / pieces, e = i % pieces * 4, row = row_tile * a.tile_rows + r;
   const bool here = r < a.tile_rows && row < v.t * a.G;
   float peak = kLowest, sums = 0.0f;
+  bool broken = false;  // a part's maximum that is a NaN: the row is left alone
   float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
   // (a part that has seen nothing has weight zero, not zero times what it holds)
   auto add = [&](float2 m, float4v x, float now) {
@@ -824,6 +835,7 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
         const int64_t part = (part0 + min(c + u * kGroups, parts - 1)) * a.tile_rows + r;
         m[u] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part);
         x[u] = *reinterpret_cast<const float4v *>(a.part_o + part * (8 * p.d8) + e);
+        broken = broken || m[u].x != m[u].x;
         if (c + u * kGroups >= parts) m[u] = make_float2(kLowest, 0.0f);
       }
       float now = peak;
@@ -840,9 +852,12 @@ __global__ __launch_bounds__(kBlock) void join_kernel(AttendArgs a) {
     }
   }
   meet_o[threadIdx.x] = o;
-  meet_ml[threadIdx.x] = make_float2(peak, sums);
+  meet_ml[threadIdx.x] = make_float2(broken ? __builtin_nanf("") : peak, sums);
   __syncthreads();
   if (group != 0 || !here) return;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) broken = broken || meet_ml[threadIdx.x + g * kLanes].x != meet_ml[threadIdx.x + g * kLanes].x;
+  if (broken) return;
 #pragma unroll
   for (int g = 1; g < kGroups; ++g) peak = fmaxf(peak, meet_ml[threadIdx.x + g * kLanes].x);
   sums = 0.0f;

@@ -592,3 +592,45 @@ def test_many_small_weights_beside_a_large_one(dtype):
     off = (got.double().cpu() - want).abs()
     assert bool((off <= tol).all()), float((off / tol).max())
     assert bool(((lse.double().cpu() - (gap + (1 + small).log())[:, None]).abs() <= ((n + t) / 32 + 64) * u).all())
+
+
+@pytest.mark.parametrize("d,G,t,n", [(64, 1, 6, 40), (128, 8, 6, 300), (64, 20, 6, 500), (256, 20, 6, 300), (128, 1, 6, 5000),
+                                     (128, 8, 6, 9000), (128, 20, 6, 20011), (256, 9, 6, 9000), (200, 20, 6, 9000)])
+def test_rows_of_broken_sessions_are_left_alone(d, G, t, n):
+    """A page that is none, wherever in the context, or a parent that is none: the session's rows stay as they were, those of
+    the others are what they are without it, and so is the next call's result."""
+    H, B = 2, 16
+    cache, _ = make(torch.float16, d, H, B, [n, n // 2 + t, n], seed=d + G)
+    q = torch.randn((3 * t, H * G, d), device=DEV).to(torch.float16)
+    off, tree = offsets([t] * 3), random_tree(random.Random(n), t) * 3
+
+    def call(parents):
+        out, lse = torch.full_like(q, 5.0), torch.full((3 * t, H * G), 5.0, device=DEV)
+        cache.attend(q, off, parents=ints(parents), max_nodes=t, max_len=n, out=out, lse=lse)
+        return out, lse
+
+    clean = call(tree)
+    cache.check_status()
+
+    def check_broken(got, s):
+        with pytest.raises(plc.PlcError) as e:
+            cache.check_status()
+        assert e.value.code == plc.PLC_ERR_INVALID
+        here = slice(s * t, (s + 1) * t)
+        for x, y in zip(got, clean):
+            assert (x[here] == 5).all()
+            assert torch.equal(x[: here.start], y[: here.start]) and torch.equal(x[here.stop:], y[here.stop:])
+        assert all(torch.equal(x, y) for x, y in zip(call(tree), clean))
+        cache.check_status()
+
+    for s, slot in ((0, 0), (1, (n // 2 + t - 1) // B), (2, n // B // 2), (2, (n - 1) // B)):
+        for page in (-1, cache.P, 2**31 - 1):
+            was = int(cache.table[s, slot])
+            cache.table[s, slot] = page
+            got = call(tree)
+            cache.table[s, slot] = was
+            check_broken(got, s)
+    for s, node, parent in ((0, 0, 0), (1, 3, 4), (2, t - 1, -2)):
+        parents = list(tree)
+        parents[s * t + node] = parent
+        check_broken(call(parents), s)
