@@ -671,8 +671,9 @@ int plc_pages_trim(const plc_pages *pages, const int32_t *new_lens, uint32_t *st
 /* Keeps the accepted nodes of a drafted tree: the session's last t positions are the tree's nodes (`off`), and
  * path[path_off[s] .. path_off[s+1]) the numbers of those to keep, strictly ascending.  Their rows move, in all
  * layers, to the first positions of the tree; the session ends behind them, pages that it no longer reaches are
- * given back.  The pages that are written must be the session's own (plc_pages_extend has made them so), else
- * status PLC_ERR_INVALID is raised and they are left alone. */
+ * given back.  The pages that are written must be the session's own (plc_pages_extend has made them so).  Where
+ * they are not, or the path is not as described, status PLC_ERR_INVALID is raised and the session stays as it was, its
+ * length and pages too. */
 int plc_pages_accept(const plc_pages *pages, const int32_t *off, const int32_t *path, int64_t path_len,
                      const int32_t *path_off, uint32_t *status, void *stream);
 

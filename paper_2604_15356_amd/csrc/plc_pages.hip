@@ -295,7 +295,7 @@ __global__ __launch_bounds__(kBlock) void trim_kernel(PoolView p, const int32_t 
   trim_session<kBlock>(p, (int32_t)blockIdx.x, new_lens[blockIdx.x], status);
 }
 
-// The nodes of a session's tree that are kept: checked, as both kernels of plc_pages_accept need them.
+// The nodes of a session's tree that are kept: checked, as the kernels of plc_pages_accept need them.
 struct Accepted {
   int32_t t, m, first;  // nodes, accepted ones, the first of them in `path`
   int64_t ctx;          // positions in front of the tree
@@ -311,12 +311,51 @@ __device__ __forceinline__ Accepted accepted_of(const PoolView &p, int32_t s, co
   return a;
 }
 
-__global__ __launch_bounds__(kBlock) void accept_trim_kernel(PoolView p, const int32_t *__restrict__ off,
-                                                             const int32_t *__restrict__ path_off, int64_t path_len,
-                                                             uint32_t *status) {
-  const Accepted a = accepted_of(p, (int32_t)blockIdx.x, off, path_off, path_len);
-  if (a.ok) trim_session<kBlock>(p, (int32_t)blockIdx.x, a.ctx + a.m, status);
-  else if (threadIdx.x == 0) raise(status, PLC_ERR_INVALID);
+// Whether all of a session's path can be followed: its nodes ascend, the rows are on pages, and those that are written are
+// its own.  Asked by a whole workgroup, at a time when nobody gives pages back.
+template <int kThreads>
+__device__ __forceinline__ bool path_ok(const PoolView &p, int32_t s, const Accepted &a, const int32_t *path) {
+  bool ok = true;
+  for (int32_t r = threadIdx.x; r < a.m; r += kThreads) {
+    const int32_t node = path[a.first + r];
+    if (node < r || node >= a.t || (r > 0 && node <= path[a.first + r - 1])) {
+      ok = false;
+    } else if (node != r) {
+      const int64_t pf = a.ctx + node, pt = a.ctx + r;
+      const int32_t page_f = p.table[(int64_t)s * p.M + (pf >> p.shift)], page_t = p.table[(int64_t)s * p.M + (pt >> p.shift)];
+      ok = ok && p.page_ok(page_f) && p.page_ok(page_t) && p.refs[page_t] == 1;
+    }
+  }
+  return __syncthreads_and(ok);
+}
+
+// The accepted sessions' new lengths.  A session whose path cannot be followed keeps its length, and all else that it has; of
+// several sessions one could give back a page while another looks whether it is its own, so that the pages follow after this.
+__global__ __launch_bounds__(kBlock) void accept_lens_kernel(PoolView p, const int32_t *__restrict__ off,
+                                                             const int32_t *__restrict__ path, int64_t path_len,
+                                                             const int32_t *__restrict__ path_off, uint32_t *status) {
+  const int32_t s = (int32_t)blockIdx.x;
+  const Accepted a = accepted_of(p, s, off, path_off, path_len);
+  const bool ok = a.ok && path_ok<kBlock>(p, s, a, path);
+  if (threadIdx.x != 0) return;
+  if (ok) p.lens[s] = (int32_t)(a.ctx + a.m);
+  else raise(status, PLC_ERR_INVALID);
+}
+
+// Gives back what pages a session still has behind its length, up to where its tree may have ended.
+__global__ __launch_bounds__(kBlock) void accept_release_kernel(PoolView p, const int32_t *__restrict__ off, uint32_t *status) {
+  const int32_t s = (int32_t)blockIdx.x;
+  const int64_t most = (int64_t)p.M << p.shift, len = p.lens[s], t = (int64_t)off[s + 1] - off[s];
+  if (len < 0 || len > most || t < 0) return;  // (the kernel before says so)
+  const int32_t end = pages_of(min(len + t, most), p.shift);
+  for (int32_t j = pages_of(len, p.shift) + (int32_t)threadIdx.x; j < end; j += kBlock) {
+    int32_t *const entry = &p.table[(int64_t)s * p.M + j];
+    const int32_t page = *entry;
+    if (page == -1) continue;
+    *entry = -1;
+    if (p.page_ok(page)) atomicSub(&p.refs[page], 1);
+    else raise(status, PLC_ERR_INVALID);
+  }
 }
 
 // Pages in use at or above U (the number in use) go to the free ones below it: both in lists, and where page p went.
@@ -386,7 +425,7 @@ __global__ __launch_bounds__(kBlock) void move_pages_kernel(PoolView p, const Mo
   }
 }
 
-// Rows of accepted nodes to the front of the tree.  A lane owns 16 bytes of a head's row and goes through the path in
+// Rows of accepted nodes, along a path that can be followed, to the front of the tree.  A lane owns 16 bytes of a head's row and goes through the path in
 // order, several nodes at a time, all of their loads before the first of their stores: a row goes only to places whose own
 // node has been read (path[r] >= r, ascending).
 constexpr int kPathRound = 64, kPathBatch = 8;
@@ -395,7 +434,7 @@ struct PathPlaces {
 };
 template <int kThreads>
 __device__ __forceinline__ void accept_rows(const PoolView &p, int32_t s, const Accepted &a, const int32_t *path, int32_t i,
-                                            PathPlaces *places, uint32_t *status) {
+                                            PathPlaces *places) {
   const int32_t columns = 2 * p.L * p.H * p.d8;
   const int32_t c = i % p.d8, lh = i / p.d8 % (p.L * p.H);
   uint16_t *const base = (i < columns / 2 ? p.k : p.v) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)c * 8;
@@ -406,19 +445,10 @@ __device__ __forceinline__ void accept_rows(const PoolView &p, int32_t s, const 
       int64_t f = -1, t = -1;
       if (r < a.m) {
         const int32_t node = path[a.first + r];
-        const bool ascends = r == 0 || node > path[a.first + r - 1];
-        if (node < r || node >= a.t || !ascends) {
-          raise(status, PLC_ERR_INVALID);
-        } else if (node != r) {
-          const int64_t pf = a.ctx + node, pt = a.ctx + r;
-          const int32_t page_f = p.table[(int64_t)s * p.M + (pf >> p.shift)], page_t = p.table[(int64_t)s * p.M + (pt >> p.shift)];
-          const int64_t mask = (1 << p.shift) - 1;
-          if (p.page_ok(page_f) && p.page_ok(page_t) && p.refs[page_t] == 1) {
-            f = page_f * p.page_s + (pf & mask) * p.row_s;
-            t = page_t * p.page_s + (pt & mask) * p.row_s;
-          } else {
-            raise(status, PLC_ERR_INVALID);
-          }
+        if (node != r) {
+          const int64_t pf = a.ctx + node, pt = a.ctx + r, mask = (1 << p.shift) - 1;
+          f = p.table[(int64_t)s * p.M + (pf >> p.shift)] * p.page_s + (pf & mask) * p.row_s;
+          t = p.table[(int64_t)s * p.M + (pt >> p.shift)] * p.page_s + (pt & mask) * p.row_s;
         }
       }
       places->from[threadIdx.x] = f;
@@ -441,26 +471,25 @@ __device__ __forceinline__ void accept_rows(const PoolView &p, int32_t s, const 
 
 __global__ __launch_bounds__(kBlock) void accept_rows_kernel(PoolView p, const int32_t *__restrict__ off,
                                                              const int32_t *__restrict__ path, int64_t path_len,
-                                                             const int32_t *__restrict__ path_off, uint32_t *status) {
+                                                             const int32_t *__restrict__ path_off) {
   __shared__ PathPlaces places;
   const int32_t s = (int32_t)blockIdx.y;
   const Accepted a = accepted_of(p, s, off, path_off, path_len);
-  if (!a.ok) return;  // the trimming kernel says so
-  accept_rows<kBlock>(p, s, a, path, (int32_t)blockIdx.x * kBlock + (int32_t)threadIdx.x, &places, status);
+  if (!a.ok || !path_ok<kBlock>(p, s, a, path)) return;  // the next kernel says so
+  accept_rows<kBlock>(p, s, a, path, (int32_t)blockIdx.x * kBlock + (int32_t)threadIdx.x, &places);
 }
 
-// Both at once, for a single session of rows so short that one workgroup has them: a launch less.  (Of several sessions one
-// could give back a page while another looks whether it is its own.)
+// All at once, for a single session of rows so short that one workgroup has them: two launches less.
 __global__ __launch_bounds__(kManager) void accept_kernel(PoolView p, const int32_t *__restrict__ off,
                                                           const int32_t *__restrict__ path, int64_t path_len,
                                                           const int32_t *__restrict__ path_off, uint32_t *status) {
   __shared__ PathPlaces places;
   const Accepted a = accepted_of(p, 0, off, path_off, path_len);
-  if (!a.ok) {
+  if (!a.ok || !path_ok<kManager>(p, 0, a, path)) {
     if (threadIdx.x == 0) raise(status, PLC_ERR_INVALID);
     return;
   }
-  for (int32_t i = 0; i < 2 * p.L * p.H * p.d8; i += kManager) accept_rows<kManager>(p, 0, a, path, i + (int32_t)threadIdx.x, &places, status);
+  for (int32_t i = 0; i < 2 * p.L * p.H * p.d8; i += kManager) accept_rows<kManager>(p, 0, a, path, i + (int32_t)threadIdx.x, &places);
   __syncthreads();
   trim_session<kManager>(p, 0, a.ctx + a.m, status);
 }
@@ -650,8 +679,9 @@ extern "C" int plc_pages_accept(const plc_pages *pages, const int32_t *off, cons
   }
   if (path_len > 0)
     hipLaunchKernelGGL(accept_rows_kernel, dim3((unsigned)((columns + kBlock - 1) / kBlock), (unsigned)p.S), dim3(kBlock), 0,
-                       st, p, off, path, path_len, path_off, status);
-  hipLaunchKernelGGL(accept_trim_kernel, dim3((unsigned)p.S), dim3(kBlock), 0, st, p, off, path_off, path_len, status);
+                       st, p, off, path, path_len, path_off);
+  hipLaunchKernelGGL(accept_lens_kernel, dim3((unsigned)p.S), dim3(kBlock), 0, st, p, off, path, path_len, path_off, status);
+  hipLaunchKernelGGL(accept_release_kernel, dim3((unsigned)p.S), dim3(kBlock), 0, st, p, off, status);
   return launch_status();
 }
 

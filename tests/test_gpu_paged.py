@@ -407,3 +407,47 @@ def test_more_room_than_32_bits_count(S):
     cache.extend(ints([1, 1] + [0] * (S - 2)))  # what there is room for is still given
     cache.check_status()
     assert lens.tolist() == [6, 6] + [0] * (S - 2) and refs.tolist() == [1, 0, 0, 1, 0, 0] and table[:2, 0].tolist() == [0, 3]
+
+
+@pytest.mark.parametrize("L,H,d,sessions", [(2, 2, 16, 1), (9, 8, 128, 1), (2, 2, 16, 4), (9, 8, 128, 4)])
+@pytest.mark.parametrize("path", [[0, 0], [5, 3], [2, 40], [-1], [0, 2, 30, 31, 33, 34, 35, 36, 37, 36], list(range(1, 38))])
+def test_a_refused_path_changes_nothing(L, H, d, sessions, path):
+    """Every form of the call: a path that cannot be followed, wherever it breaks off, leaves its session's rows, length, pages
+    and counts; the other sessions' are accepted."""
+    t, B = 37, 16
+    cache = make(12 * sessions, L, H, B, d, sessions, 6)
+    model = Model(cache)
+    lens = [60 + i for i in range(sessions)]
+    cache.extend(ints(lens))
+    model.extend(lens)
+    good = [1, 2, 20, 36]
+    for s in range(sessions):
+        cache.accept(offsets([t] * sessions), ints(good * s + path + good * (sessions - 1 - s)),
+                     offsets([len(good)] * s + [len(path)] + [len(good)] * (sessions - 1 - s)))
+        with pytest.raises(plc.PlcError) as e:
+            cache.check_status()
+        assert e.value.code == plc.PLC_ERR_INVALID
+        kept = [list(range(t)) if i == s else good for i in range(sessions)]
+        model.accept([t] * sessions, kept)
+        model.check(cache)
+        grow = [lens[i] - n for i, n in enumerate(model.lens)]
+        cache.extend(ints(grow))
+        model.extend(grow)
+
+
+def test_a_page_given_back_in_the_call_was_not_the_sessions_own():
+    """Two sessions on the same pages: one gives up all of its tree, which would leave the pages to the other alone; but it is
+    not to write on them in this call, in whatever order the sessions come."""
+    for turned in (False, True):
+        cache = make(12, 2, 2, 16, 16, 2, 4)
+        model = Model(cache)
+        cache.extend(ints([40, 0]))
+        model.extend([40, 0])
+        cache.fork(ints([0, 0]))
+        model.fork([0, 0])
+        paths = [[], [1, 3]][:: -1 if turned else 1]
+        cache.accept(offsets([24, 24]), ints([1, 3]), offsets([len(p) for p in paths]))
+        with pytest.raises(plc.PlcError):
+            cache.check_status()
+        model.accept([24, 24], [[] if not p else list(range(24)) for p in paths])
+        model.check(cache)
