@@ -636,7 +636,7 @@ typedef struct plc_pages {
   int64_t stride[4];      /* element strides of (page, layer, head, row), multiples of 8; components are
                              contiguous                                                                  */
   int32_t P, L, H, B, d;  /* pages, layers, KV heads, rows of a page (a power of two, 16..1024), components
-                             (a multiple of 8)                                                           */
+                             (a multiple of 8); L * H * 2 d < 2^31, B times the row's stride < 2^30      */
   int32_t S, M;           /* sessions (1..1024), entries of a session (M * B <= 2^30)                    */
   int32_t *table, *lens, *refs;
 } plc_pages;
@@ -645,7 +645,7 @@ typedef struct plc_rows {
   int32_t layer, layers;  /* the pool's layers layer .. layer + layers-1                                 */
   int32_t packed;         /* 1: row x of the call is row x of the buffer, sessions one behind the other;
                              0: row i of session s is row i of the session's part of the buffer          */
-  int64_t rows;           /* rows of the buffer (packed) or of each session's part                       */
+  int64_t rows;           /* rows of the buffer (packed) or of each session's part; below 2^31         */
   int64_t stride[4];      /* element strides of (session, layer, head, row), multiples of 8; that of the
                              session is not used with packed                                             */
 } plc_rows;
@@ -702,7 +702,8 @@ int plc_pages_load(const plc_pages *pages, const plc_rows *rows, const int32_t *
  * down to 2^-21 of the largest keep all of the type's bits).  Rows that a node does
  * not see have no effect on it, whatever they hold; an infinity or a NaN in v reaches whoever sees it, however small its weight.  Sessions without nodes take no part.
  *   layer      0..L-1.
- *   type       PLC_FP16 or PLC_BF16, of the cache, q and out.  d <= 256.
+ *   type       PLC_FP16 or PLC_BF16, of the cache, q and out.  d <= 256, H * G <= 65536, max_nodes * G < 2^23, the pool's
+ *              row stride < 2^25; S * H * max_nodes * G / 32 in all, times the pieces that contexts are cut into, < 2^31.
  *   q, out     logical [N, H*G, d], element strides (node, head) in q_stride / out_stride, multiples of 8;
  *              16-byte aligned.  Node x of the call is row x; rows behind off[S] are left alone.
  *   off        as above, off[S] <= N.

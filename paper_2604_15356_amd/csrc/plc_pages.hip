@@ -495,7 +495,7 @@ __global__ __launch_bounds__(kManager) void accept_kernel(PoolView p, const int3
 }
 
 // Rows between a caller's buffer and pages.  A workgroup takes a block of consecutive rows, as many as give each thread 16
-// bytes of one head, works out where they are, and goes through a run of heads.
+// bytes of one head, works out where they are, and goes through runs of heads: one, up to the 65,535 that a grid is wide.
 constexpr int kHeadRun = 4;
 struct RowsView {
   uint16_t *k, *v;
@@ -554,18 +554,17 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, co
     in_buf[b] = buf;
   }
   __syncthreads();
-  const int32_t heads = r.layers * p.H, lh0 = (int32_t)blockIdx.y * kHeadRun, lh1 = min(lh0 + kHeadRun, heads);
-  const int32_t items = r.per_block * p.d8;
+  const int32_t heads = r.layers * p.H, items = r.per_block * p.d8;
   for (int32_t i = threadIdx.x; i < items; i += kBlock) {
     const int32_t b = i / p.d8, c = i - b * p.d8;
     if (in_pool[b] < 0) continue;
     const int64_t pool = in_pool[b] + r.layer * p.layer_s + (int64_t)c * 8, buf = in_buf[b] + (int64_t)c * 8;
-    for (int32_t lh = lh0; lh < lh1; lh += 4) {
+    for (int32_t lh = (int32_t)blockIdx.y * kHeadRun; lh < heads; lh += (int32_t)gridDim.y * kHeadRun) {
       uint4 k[4], v[4];
       int64_t to[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int32_t e = min(lh + u, lh1 - 1), l = e / p.H, h = e - l * p.H;
+        const int32_t e = min(lh + u, heads - 1), l = e / p.H, h = e - l * p.H;
         const int64_t at_pool = pool + l * p.layer_s + h * p.head_s, at_buf = buf + l * r.layer_s + h * r.head_s;
         k[u] = get16<kStream>((kStore ? r.k : p.k) + (kStore ? at_buf : at_pool));
         v[u] = get16<kStream>((kStore ? r.v : p.v) + (kStore ? at_buf : at_pool));
@@ -573,7 +572,7 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, co
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        if (lh + u < lh1) {
+        if (lh + u < heads) {
           put16<kStream>((kStore ? p.k : r.k) + to[u], k[u]);
           put16<kStream>((kStore ? p.v : r.v) + to[u], v[u]);
         }
@@ -611,11 +610,12 @@ int move_rows(bool store, const plc_pages *pages, const plc_rows *rows, const in
   r.layer = rows->layer, r.layers = rows->layers, r.packed = rows->packed;
   r.per_block = p.d8 >= kBlock ? 1 : kBlock / p.d8;
   const int64_t total = rows->packed ? rows->rows : rows->rows * pages->S;
-  const int64_t bx = (total + r.per_block - 1) / r.per_block, by = ((int64_t)r.layers * p.H + kHeadRun - 1) / kHeadRun;
-  if (bx > INT32_MAX || by > 65535) return PLC_ERR_INVALID;
+  const int64_t bx = (total + r.per_block - 1) / r.per_block, heads = (int64_t)r.layers * p.H,
+                by = (heads + kHeadRun - 1) / kHeadRun;
+  if (bx > INT32_MAX) return PLC_ERR_INVALID;
   const size_t lds = 16 * (size_t)r.per_block + 4 * (size_t)(p.S + 1);
-  const dim3 grid((unsigned)bx, (unsigned)by);
-  const bool stream = total * r.layers * p.H * p.d8 * 64 > kCached;  // of both halves, in and out
+  const dim3 grid((unsigned)bx, (unsigned)(by < 65535 ? by : 65535));
+  const bool stream = (double)total * heads * p.d8 * 64 > (double)kCached;  // of both halves, in and out
   const auto kernel = !store ? &rows_kernel<false, false> : stream ? &rows_kernel<true, true> : &rows_kernel<true, false>;
   hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, st, p, r, off, status);
   return launch_status();

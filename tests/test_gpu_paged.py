@@ -451,3 +451,22 @@ def test_a_page_given_back_in_the_call_was_not_the_sessions_own():
             cache.check_status()
         model.accept([24, 24], [[] if not p else list(range(24)) for p in paths])
         model.check(cache)
+
+
+def test_more_heads_than_a_grid_is_wide():
+    L, H, B, d = 300, 1024, 16, 8
+    torch.manual_seed(2)
+    cache = make(3, L, H, B, d, 2, 2)
+    cache.extend(ints([20, 3]))
+    before = cache.k.clone()
+    k, v = rows_like(cache, 7, L)
+    cache.store(k, v, offsets([5, 2]))
+    out, out2 = torch.zeros_like(k), torch.zeros_like(v)
+    cache.load(out, out2, offsets([5, 2]))
+    cache.check_status()
+    assert torch.equal(out, k) and torch.equal(out2, v)
+    t = cache.table.tolist()
+    for i, (page, row) in enumerate([(t[0][0], 15), (t[0][1], 0), (t[0][1], 1), (t[0][1], 2), (t[0][1], 3), (t[1][0], 1), (t[1][0], 2)]):
+        assert torch.equal(cache.k[page, :, :, row], k[i])
+        before[page, :, :, row] = k[i]
+    assert torch.equal(cache.k, before)
