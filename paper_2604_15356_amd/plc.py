@@ -535,6 +535,8 @@ def make_pages(k, v, table, lens, refs) -> plc_pages:
         raise TypeError(f"expected float16 or bfloat16, got {k.dtype}")
     if table.dim() != 2 or lens.shape != table.shape[:1] or refs.shape != k.shape[:1]:
         raise ValueError("table [sessions, entries], lens [sessions], refs [pages]")
+    if len({t.device for t in (k, v, table, lens, refs)}) != 1:
+        raise ValueError("k, v, table, lens and refs are on one device")
     pages = plc_pages()
     pages.k, pages.v = _ptr(k), _ptr(v)
     pages.stride = (C.c_int64 * 4)(*k.stride()[:4])
@@ -551,8 +553,16 @@ def plc_pages_workspace_bytes(pages) -> int:
 # The calls of the paged cache come once or more a token, and last as long as a launch or two: their arguments go over as
 # plain addresses, and the stream is asked for directly.
 _I64x2 = C.c_int64 * 2
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _int32 = torch.int32
+
+
+def _stream_of(t):
+    """The current stream, of the device that launches go to: tensors of another are not for it."""
+    device = t.get_device()
+    if device != _current_device():
+        raise ValueError(f"plc works on the current device, {_current_device()}; the tensors are on {device}")
+    return _raw_stream(device)
 
 
 def _ints(t):
@@ -573,28 +583,28 @@ def _on_device(t):
 
 def plc_pages_fork(pages, src, status):
     """src int32 [S]: what each session becomes; -1: empty."""
-    _check(lib().plc_pages_fork(pages, _ints(src), _ints(status), _raw_stream(src.device.index)), "plc_pages_fork")
+    _check(lib().plc_pages_fork(pages, _ints(src), _ints(status), _stream_of(src)), "plc_pages_fork")
 
 
 def plc_pages_extend(pages, grow, ws, status):
     _check(lib().plc_pages_extend(pages, _ints(grow), _on_device(ws), ws.numel(), _ints(status),
-                                  _raw_stream(grow.device.index)), "plc_pages_extend")
+                                  _stream_of(grow)), "plc_pages_extend")
 
 
 def plc_pages_trim(pages, new_lens, status):
-    _check(lib().plc_pages_trim(pages, _ints(new_lens), _ints(status), _raw_stream(new_lens.device.index)), "plc_pages_trim")
+    _check(lib().plc_pages_trim(pages, _ints(new_lens), _ints(status), _stream_of(new_lens)), "plc_pages_trim")
 
 
 def plc_pages_accept(pages, off, path, path_off, status):
     """off, path_off int32 [S+1]; path int32: numbers of the nodes to keep, ascending in each session."""
     _check(lib().plc_pages_accept(pages, _ints(off), _ints(path), path.numel(), _ints(path_off), _ints(status),
-                                  _raw_stream(off.device.index)), "plc_pages_accept")
+                                  _stream_of(off)), "plc_pages_accept")
 
 
 def plc_pages_compact(pages, used, ws, status):
     """used int32 [1] out, or None: pages in use."""
     _check(lib().plc_pages_compact(pages, None if used is None else _ints(used), _on_device(ws), ws.numel(), _ints(status),
-                                   _raw_stream(ws.device.index)), "plc_pages_compact")
+                                   _stream_of(ws)), "plc_pages_compact")
 
 
 _rows_known = {}  # descriptions of rows by their layout
@@ -620,13 +630,13 @@ def _rows_of(k, v, layer):
 def plc_pages_store(pages, off, k, v, layer, status):
     """k, v [rows, layers, H, d] packed, or [S, layers, H, rows, d]; off int32 [S+1]; layer: the first of the pool's."""
     _check(lib().plc_pages_store(pages, _rows_of(k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
-                                 _raw_stream(off.device.index)), "plc_pages_store")
+                                 _stream_of(off)), "plc_pages_store")
 
 
 def plc_pages_load(pages, off, k, v, layer, status):
     """plc_pages_store the other way round."""
     _check(lib().plc_pages_load(pages, _rows_of(k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
-                                _raw_stream(off.device.index)), "plc_pages_load")
+                                _stream_of(off)), "plc_pages_load")
 
 
 def plc_attend_workspace_bytes(pages, G, N, max_nodes, max_len) -> int:
@@ -651,7 +661,7 @@ def plc_attend(pages, layer, q, off, parents, max_nodes, max_len, scale, out, ls
                             shape[1] // pages.H, shape[0], _ints(off), None if parents is None else _ints(parents), max_nodes,
                             max_len, scale, out.data_ptr(), q_stride if os_ == qs else _I64x2(os_[0], os_[1]),
                             None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _ints(status),
-                            _raw_stream(q.get_device())), "plc_attend")
+                            _stream_of(q)), "plc_attend")
 
 
 class PrefixTrie:

@@ -141,3 +141,35 @@ def test_tensors_that_the_binding_refuses():
             plc.plc_attend(g, 0, bad_q, ints(4), None, 5, 64, 1.0, bad_q, None, ints(256), ints(1))
     with pytest.raises(TypeError):
         plc.plc_attend(g, 0, q.float(), ints(4), None, 5, 64, 1.0, q.float(), None, ints(256), ints(1))
+
+
+class Elsewhere:
+    """What the binding looks at of a tensor on device 1."""
+    is_cuda, device = True, torch.device("cuda", 1)
+
+    def __init__(self, dtype=torch.int32, shape=(4,)):
+        self.dtype, self.shape = dtype, torch.Size(shape)
+        self.stride = torch.empty(shape).stride
+
+    is_contiguous = lambda self: True  # noqa: E731
+    data_ptr = lambda self: 4096  # noqa: E731
+    get_device = lambda self: 1  # noqa: E731
+    numel = lambda self: self.shape.numel()  # noqa: E731
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The stream that a call takes is the current device's, as is the launch."""
+    monkeypatch.setattr(plc, "_current_device", lambda: 0, raising=False)
+    i, g = Elsewhere(), _pages()
+    rows, q = Elsewhere(torch.float16, (5, 2, 2, 64)), Elsewhere(torch.float16, (5, 4, 64))
+    ws = Elsewhere(torch.uint8, (1 << 20,))
+    for call in (lambda: plc.plc_pages_fork(g, i, i), lambda: plc.plc_pages_extend(g, i, ws, i), lambda: plc.plc_pages_trim(g, i, i),
+                 lambda: plc.plc_pages_accept(g, i, i, i, i), lambda: plc.plc_pages_compact(g, None, ws, i),
+                 lambda: plc.plc_pages_store(g, i, rows, rows, 0, i), lambda: plc.plc_pages_load(g, i, rows, rows, 0, i),
+                 lambda: plc.plc_attend(g, 0, q, i, None, 5, 64, 1.0, q, None, ws, i)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    k, ints = Elsewhere(torch.float16, (4, 2, 2, 16, 64)), lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    k.dim, table = lambda: 5, ints(3, 2)
+    with pytest.raises(ValueError, match="one device"):
+        plc.make_pages(k, k, table, ints(3), ints(4))
