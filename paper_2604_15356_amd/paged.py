@@ -80,9 +80,6 @@ class PagedKVCache:
             k, v = k.unsqueeze(1), v.unsqueeze(1)
         if k.dtype is not self.dtype or v.dtype is not self.dtype:
             raise TypeError(f"expected {self.dtype}, got {k.dtype} and {v.dtype}")
-        shape = k.shape
-        if len(shape) not in (4, 5) or shape[2] != self.H or shape[-1] != self.d or (len(shape) == 5 and shape[0] != self.S):
-            raise ValueError("rows are [rows, layers, H, d] packed, [rows, H, d] of one layer, or [S, layers, H, rows, d]")
         return k, v, layer
 
     def store(self, k, v, off, layer=0):

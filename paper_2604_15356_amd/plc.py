@@ -610,32 +610,36 @@ def plc_pages_compact(pages, used, ws, status):
 _rows_known = {}  # descriptions of rows by their layout
 
 
-def _rows_of(k, v, layer):
+def _rows_of(pages, k, v, layer):
     """Rows in a buffer: packed [rows, layers, heads, d], or [S, layers, heads, rows, d], of any strides but the last."""
     st, shape = k.stride(), k.shape
     if shape != v.shape or k.dtype is not v.dtype or st != v.stride():
         raise ValueError("k and v are [rows, layers, heads, d] or [sessions, layers, heads, rows, d] of one layout")
-    rows = _rows_known.get((shape, st, layer))
+    rows = _rows_known.get((shape, st, layer, k.dtype))
     if rows is None:
         if len(shape) not in (4, 5) or st[-1] != 1:
             raise ValueError("k and v are [rows, layers, heads, d] or [sessions, layers, heads, rows, d] of one layout")
+        if k.dtype is not torch.float16 and k.dtype is not torch.bfloat16:
+            raise TypeError(f"expected float16 or bfloat16, got {k.dtype}")
         if len(_rows_known) >= 1024:
             _rows_known.clear()
         rows = plc_rows(layer, shape[1], 1, shape[0], (0, st[1], st[2], st[0])) if len(shape) == 4 else \
             plc_rows(layer, shape[1], 0, shape[3], st[:4])
-        _rows_known[shape, st, layer] = rows
+        _rows_known[shape, st, layer, k.dtype] = rows
+    if shape[2] != pages.H or shape[-1] != pages.d or (len(shape) == 5 and shape[0] != pages.S):
+        raise ValueError("rows have the pool's heads and components, and a part for each of its sessions")
     return rows
 
 
 def plc_pages_store(pages, off, k, v, layer, status):
     """k, v [rows, layers, H, d] packed, or [S, layers, H, rows, d]; off int32 [S+1]; layer: the first of the pool's."""
-    _check(lib().plc_pages_store(pages, _rows_of(k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
+    _check(lib().plc_pages_store(pages, _rows_of(pages, k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
                                  _stream_of(off)), "plc_pages_store")
 
 
 def plc_pages_load(pages, off, k, v, layer, status):
     """plc_pages_store the other way round."""
-    _check(lib().plc_pages_load(pages, _rows_of(k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
+    _check(lib().plc_pages_load(pages, _rows_of(pages, k, v, layer), _ints(off), _on_device(k), _on_device(v), _ints(status),
                                 _stream_of(off)), "plc_pages_load")
 
 

@@ -173,3 +173,17 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     k.dim, table = lambda: 5, ints(3, 2)
     with pytest.raises(ValueError, match="one device"):
         plc.make_pages(k, k, table, ints(3), ints(4))
+
+
+def test_rows_of_another_shape_or_type_than_the_pools_are_refused(monkeypatch):
+    monkeypatch.setattr(plc, "_current_device", lambda: 0, raising=False)
+    g, i = _pages(), Elsewhere()
+    for shape in ((5, 2, 3, 64), (5, 2, 2, 72), (5, 2, 2, 32), (4, 2, 2, 5, 64), (3, 2, 4, 5, 64), (3, 2, 2, 5, 80), (5, 2, 64)):
+        rows = Elsewhere(torch.float16, shape)
+        for call in (plc.plc_pages_store, plc.plc_pages_load):
+            with pytest.raises(ValueError, match="rows"):
+                call(g, i, rows, rows, 0, i)
+    rows = Elsewhere(torch.float32, (5, 2, 2, 64))
+    for call in (plc.plc_pages_store, plc.plc_pages_load):
+        with pytest.raises(TypeError):
+            call(g, i, rows, rows, 0, i)
