@@ -16,11 +16,12 @@
 // cut where they are long, or where there are few rows and heads to fill the chip with (attend_plan has the rule).
 // Workgroups take the chunks in turn; what a cut has split is joined by a second kernel.
 //
-// What bounds it: few rows, HBM (64 sessions of one token, 8 heads, 4 query heads each, up to 4096 positions: 547 MB in
-// 111 us, 4.9 TB/s; a copy of 4 GB reaches 4.9).  Many rows, the turns of the matrix cores and the vector units (64 nodes,
-// 32,768 positions: 34 GFLOP in 60 us with the joining, 0.57 PFLOP/s; the matrix cores are busy 0.35 of the kernel's 51 us,
-// vector instructions are issued in 0.39, a third of their time the wavefronts wait at barriers and for LDS).  Short contexts,
-// the 4 us from a workgroup's start to its first products (offsets, table, pages, one after the other) and 3.5 us of its end.
+// What bounds it: few rows, HBM (64 sessions of one token, 8 heads, 4 query heads each, all of 4096 positions: 1.07 GB in
+// 188 us, 5.7 TB/s; with lengths evenly up to 4096 547 MB in 114 us, 4.8 TB/s, the longest one ends last).  Many rows, the turns
+// of the matrix cores and the vector units (64 nodes, 32,768 positions: 34 GFLOP in 60 us with the joining, 0.57 PFLOP/s; the
+// matrix cores are busy 0.34 of the kernel's 52 us, vector instructions are issued in 0.40, a third of their time the wavefronts
+// wait at barriers and for LDS; a chain of 2048 nodes after 8192 positions 504 us, 0.68 PFLOP/s).  Short contexts, the 4 us
+// from a workgroup's start to its first products (offsets, table, pages, one after the other) and 4 to 5 us of its end.
 #include <atomic>
 #include <type_traits>
 
@@ -104,8 +105,9 @@ __device__ __forceinline__ Line draw_line(const AttendArgs &a, uint32_t *line, b
     uint32_t units = max(1u, (n + kComputeUnits - 1) / kComputeUnits);
     // No more long chunks than compute units: the ones left over would be a round of their own.  A tile and head's last chunk
     // is shorter than the others, so that the first length leaves too many; a few steps come close enough, with quotients that
-    // need not be exact.  (20 sessions of up to 24,323 positions, 8 heads: 130 against 168 us.  Of short chunks a step costs
-    // more than it gains; beyond 64 sessions the first length does.)
+    // need not be exact.  (20 sessions of 24,323 positions, 8 heads: 341 against 433 us.  Of short chunks it makes no difference:
+    // 5 sessions of up to 4095 positions with trees of 27 nodes 30.3 and 30.5 us.  Beyond 64 sessions, of which a wavefront has
+    // not all in its registers, the first length is taken.)
     if (units > 3 && a.p.S <= 64) {
 #pragma unroll 1
       for (int step = 0; step < 4; ++step) {
@@ -893,8 +895,11 @@ AttendPlan attend_plan(const plc_pages *p, int32_t G, int32_t max_nodes, int32_t
   // A chunk is a workgroup's work, and a workgroup's LDS a compute unit's.  Whole positions of a tile of rows and head need no
   // joining (a launch, 5 us), and where there is one for every compute unit nothing is gained by cutting them: 64 sessions x 8
   // heads of up to 4000 positions 108 us, cut in two 121 us.  Fewer are cut into as many chunks as there are compute units, of
-  // a length that the kernels find from the sessions' own.  Short ones are quicker done by one workgroup (500 positions 7.7
-  // against 10.1 us, 1000 positions 10.8 against 9.8).
+  // a length that the kernels find from the sessions' own.  Short ones are quicker done by one workgroup: 8 heads of 4 rows, 600
+  // positions 11.6 against 12.2 us, 800 positions 13.4 against 12.2; of 64 rows, 300 positions 15.1 against 16.1, 500 positions
+  // 19.2 against 17.3; of 128 rows 21.4 against 21.0 and 25.9 against 20.8.  With more than half as many tiles and heads as compute
+  // units (160), contexts of equal lengths are better whole (2400 positions 33.7 against 36.6 us), but the host does not know
+  // them equal: evenly up to 1600 21.0 against 21.4, up to 2400 27.1 against 26.4.
   const int64_t enough = plan.rows == 32 ? 768 : 384;
   if (max_len > (2 * pairs > kComputeUnits ? 1536 : enough) && pairs < kComputeUnits) {
     plan.chunk = 0;

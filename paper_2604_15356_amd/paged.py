@@ -70,7 +70,8 @@ class PagedKVCache:
                              self._per_session(path_off, self.S + 1, "path_off"), self.status)
 
     def compact(self):
-        """Moves the pages in use to the pool's front; their number, int32 [1], on the device."""
+        """Moves the pages in use to the pool's front; their number, int32 [1], on the device, until the
+        next call of it."""
         plc.plc_pages_compact(self.pages, self.used, self.ws, self.status)
         return self.used
 
