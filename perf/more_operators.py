@@ -350,12 +350,12 @@ def _place(st, s, pos):
 
 
 def _rotated(x, positions, c, sign=1.0):
-    """x [rows, ..., d] at positions [rows], in 32 bits; the angles in 64."""
+    """x [rows, ..., d] at positions [rows], in 32 bits; the angles in 64.  sign -1: back."""
     theta, magnitude = _angles(c)
     theta = torch.tensor(theta, dtype=torch.float64, device=x.device)
     angle = sign * positions.double()[:, None] * theta
     shape = (x.shape[0],) + (1,) * (x.dim() - 2) + (-1,)
-    cos, sin = ((f(angle) * magnitude).float().view(shape) for f in (torch.cos, torch.sin))
+    cos, sin = ((f(angle) * magnitude ** sign).float().view(shape) for f in (torch.cos, torch.sin))
     r, y = c["r"], x.float()
     a, b = (y[..., 0:r:2], y[..., 1:r:2]) if c["interleaved"] else (y[..., : r // 2], y[..., r // 2:r])
     pairs = torch.stack((a * cos - b * sin, b * cos + a * sin), -1 if c["interleaved"] else -2)
@@ -506,7 +506,7 @@ def _turned(x, positions, c, sign=1):
     """Rotated by complex multiplication."""
     theta, magnitude = _angles(c)
     angle = sign * positions.double()[:, None] * torch.tensor(theta, dtype=torch.float64, device=x.device)
-    by = torch.polar(torch.full_like(angle, magnitude), angle)
+    by = torch.polar(torch.full_like(angle, magnitude ** sign), angle)
     r, out = c["r"], x.double()
     at = torch.arange(r // 2, device=x.device)
     re, im = (2 * at, 2 * at + 1) if c["interleaved"] else (at, at + r // 2)
