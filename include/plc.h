@@ -728,6 +728,136 @@ int plc_attend(const plc_pages *pages, int32_t layer, int32_t type, const void *
                void *ws, size_t ws_bytes, uint32_t *status, void *stream);
 
 /*
+ * ---- Rotary positions --------------------------------------------------------------
+ * Pair i (of r / 2) of a row at position p turns by the angle a = p * theta_i:
+ *   (x, y)  ->  magnitude * (x cos a - y sin a,  y cos a + x sin a),
+ * the pairs being components (i, i + r/2), or (2i, 2i + 1) with `interleaved`; components r and above stay as they are.
+ * The angle is taken modulo a turn in whole numbers, 2^-64 of a turn each, so that far positions lose nothing: p is any
+ * int32.  Cosine, sine and products are fp32; a result is rounded once.
+ */
+#define PLC_ROTARY_PLAIN 0     /* theta_i = base^(-2i/r)                                                          */
+#define PLC_ROTARY_LINEAR 1    /* ... / factor                                                                    */
+#define PLC_ROTARY_STRETCHED 2 /* with base * factor^(r/(r-2)) (r = 2: plain)                                     */
+#define PLC_ROTARY_PARTS 3     /* with n_i = trained * theta_i / 2 pi turns within the trained positions and
+                                  g = clamp((n_i - low) / (high - low), 0, 1):  g theta_i + (1 - g) theta_i / factor */
+#define PLC_ROTARY_RAMP 4      /* the same with 1 - g a ramp over i, from floor(at(high)) to ceil(at(low)), held within
+                                  0 .. r-1, at(n) = r ln(trained / (2 pi n)) / (2 ln base) (a ramp of no length is a
+                                  step)                                                                           */
+typedef struct plc_rotary_spec {
+  int32_t r, scaling;       /* rotated components (even, 2..2048); PLC_ROTARY_*                                   */
+  double base, factor;      /* > 0; > 1 with RAMP: base                                                           */
+  double low, high;         /* PARTS, RAMP: 0 < low < high                                                        */
+  int64_t trained;          /* PARTS, RAMP: >= 1                                                                  */
+} plc_rotary_spec;
+
+typedef struct plc_rotary {
+  const uint64_t *turns;    /* device, [r/2]: plc_rotary_turns                                                    */
+  int32_t r, interleaved;   /* rotated components (even, 2..d); 0 or 1                                            */
+  float magnitude;          /* positive, as its inverse is                                                        */
+} plc_rotary;
+
+/* theta[r/2], radians a position.  Host call, on host memory. */
+int plc_rotary_frequencies(const plc_rotary_spec *spec /* host */, double *theta /* host */);
+/* turns[pairs]: theta / 2 pi, less whole turns, in units of 2^-64.  theta finite.  Host call, on host memory. */
+int plc_rotary_turns(const double *theta /* host */, int32_t pairs, uint64_t *turns /* host */);
+
+/* Rows of a buffer: x, out logical [rows, heads, d] (element strides of row and head, multiples of 8; 16-byte aligned), out may
+ * be x, with the same strides; else they must not overlap.  positions i32 [rows].  inverse: turned by -a and divided by the
+ * magnitude.  d a multiple of 8, up to 2048; rows < 2^31, heads * d < 2^31. */
+int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x, const int64_t *x_stride /* host */,
+               int64_t rows, int32_t heads, int32_t d, const int32_t *positions, int32_t inverse, void *out,
+               const int64_t *out_stride /* host */, void *stream);
+
+/* plc_pages_store with the keys rotated on their way, and the tokens' queries too: row i of session s is at position
+ * base[s] + rel[x].
+ *   base   nullable: i32 [S]; the position of the session's first row of the call, lens[s] - t without (a cache that
+ *          plc_pages_evict has thinned out is shorter than what its session has seen).
+ *   rel    nullable: i32, one for each row of the buffer (rows, or S * rows); i without.  A drafted tree's nodes: their depths.
+ *   q, q_out   nullable, with packed rows: logical [rows->rows, H*G, d], strides (node, head) and alignment as for
+ *          plc_attend; q_out may be q, with the same strides.
+ * Rows that cannot be stored (status) are left alone, in q_out too, and so are rows behind off[S].  d up to 2048;
+ * layers * H and H * G < 2^29. */
+int plc_rotate_store(const plc_pages *pages /* host */, const plc_rows *rows /* host */, const plc_rotary *rotary /* host */,
+                     int32_t type, const int32_t *off, const int32_t *base, const int32_t *rel, const void *k, const void *v,
+                     const void *q, const int64_t *q_stride /* host */, int32_t G, void *q_out,
+                     const int64_t *q_out_stride /* host */, uint32_t *status, void *stream);
+
+/*
+ * ---- What positions have received, and eviction by it ----------------------------------
+ * A cache that may not grow keeps the positions that attention goes to.  plc_attend_weights adds up, for every position of a
+ * session, what the rows of a call give it; plc_pages_evict keeps the positions that have received most.
+ *
+ *   weights   fp32, logical [S, L, H, width] through `stride` (of session, layer, head; positions are contiguous): what
+ *             position p of a session has received in a layer and KV head.  16-byte aligned; strides and width multiples of 4, strides
+ *             (of what there is more than one of) at least the width.
+ */
+typedef struct plc_weights {
+  float *w;
+  int64_t stride[3];
+  int64_t width;  /* at least the sessions' positions */
+} plc_weights;
+
+/* With the session's last t positions, c = lens[s] - t, as a chain (node i sees the positions up to c + i), in one layer:
+ *   sum_p = sum over nodes i and query heads j of KV head h of exp(scale * q_ij . k_p - lse_ij), of those that see p;
+ *   weights[s, layer, h, p]  =  decay * weights[s, layer, h, p] + sum_p   for p < c,  sum_p  for c <= p < lens[s].
+ * (Of a drafted tree the accepted nodes alone count: after plc_pages_accept they are a chain, with their rows of q and lse.)
+ * With decay = 0 what weights hold is not read.  Positions that a row does not see take nothing from it, whatever they
+ * hold.  Products of 16-bit values accumulated in fp32, all else fp32.  The order of the sums is fixed.  Sessions without nodes
+ * take no part.
+ *   layer, type, q, q_stride, G, N, off, max_nodes, max_len, scale: as for plc_attend (max_nodes * G < 2^23).
+ *   lse      fp32 [N, H*G], as plc_attend leaves it.
+ *   decay    0..1.
+ * Where a page is none, PLC_ERR_INVALID is raised and positions on it are left alone; where a session's numbers are not as described
+ * (or it has more than `width` positions), all of its weights. */
+int plc_attend_weights(const plc_pages *pages /* host */, int32_t layer, int32_t type, const void *q,
+                       const int64_t *q_stride /* host */, int32_t G, int64_t N, const int32_t *off, int32_t max_nodes,
+                       int32_t max_len, float scale, const float *lse, float decay, const plc_weights *weights /* host */,
+                       uint32_t *status, void *stream);
+
+/* Shortens every session that has more than keep[s] positions to keep[s].  In each layer and head by itself, its first
+ * `first` and its last `last` positions stay, and of the others those with the largest weights, of equal ones the lowest
+ * positions (a NaN is larger than all numbers).  The rows that stay move, in order, to the session's first positions, and their
+ * weights with them; pages behind the new end are given back.  Rows keep the rotation that they were stored with.
+ *   keep      i32 [S], >= 0; first + last <= keep[s] where positions go.
+ *   kept      out, i32 [S, L, H, W]: the positions that stayed, ascending; min(keep[s], lens[s]) <= W of them (all of a
+ *             session's positions where none goes).  What is behind them is left alone.
+ *   max_len   host: no session has more positions.
+ *   ws        plc_pages_workspace_bytes(), 256-byte aligned.
+ * L * H < 2^22, L * H * d < 2^29.
+ * The pages from that of position `first` to that of the new end are written: they must be the session's own (a prefix that
+ * sessions share can stay, as the first positions).  Where they are not, or anything else is not as described, PLC_ERR_INVALID is
+ * raised and the session stays as it was. */
+int plc_pages_evict(const plc_pages *pages /* host */, const int32_t *keep, int32_t first, int32_t last,
+                    const plc_weights *weights /* host */, int32_t *kept, int32_t W, int32_t max_len, void *ws,
+                    size_t ws_bytes, uint32_t *status, void *stream);
+
+/*
+ * ---- What logits say of tokens -----------------------------------------------------------
+ * For every row x of logits over a vocabulary of V, with y = scale * x (scale: one over the temperature):
+ *   lse      ln sum_j exp(y_j);
+ *   logprob  y_token - lse, of the row's token (0 where that is -1: a row without one);
+ *   entropy  lse - sum_j p_j y_j, p_j = exp(y_j - lse) (terms with p_j = 0 are 0);
+ *   ids      the k largest logits' tokens, the largest first, of equal ones the lowest token first;
+ *   top_logprobs, probs   y - lse and exp(y - lse) of those: `probs` is what plc_predict_residual takes;
+ *   chosen   the token's place among them, or -1: what plc_predict_residual_cond takes.
+ * Logits may be minus infinity (masked tokens).  A row with a NaN or plus infinity, or nothing but minus infinity, raises
+ * status PLC_ERR_INVALID; its results are NaN, and ids and chosen -1.  A token that is none raises it too: logprob NaN,
+ * chosen -1.  All sums in fp32.
+ *   type     PLC_FP16, PLC_BF16 or PLC_FP32, of the logits.  Rows at `row_stride` elements, aligned as their elements are.
+ *   V        1..2^30.  N >= 0, N < 2^31.  k 0..32, at most V.
+ *   tokens   nullable: i32 [N].
+ *   logprob, entropy, lse   out, nullable: fp32 [N].  logprob, chosen: only with tokens.
+ *   ids, top_logprobs, probs, chosen   out, nullable: [N, k], chosen i32 [N].
+ *   ws       plc_score_workspace_bytes() (of any N), 256-byte aligned.
+ */
+#define PLC_FP32 2
+size_t plc_score_workspace_bytes(int32_t V, int32_t k);
+int plc_score_tokens(int32_t type, const void *logits, int64_t row_stride, int64_t N, int32_t V, float scale,
+                     const int32_t *tokens, int32_t k, float *logprob, float *entropy, float *lse, int32_t *ids,
+                     float *top_logprobs, float *probs, int32_t *chosen, void *ws, size_t ws_bytes, uint32_t *status,
+                     void *stream);
+
+/*
  * Instrumentation for benchmarks (not part of the coding path; process-wide,
  * not thread-safe).  While a pair of hipEvent_t (passed as void*) is set for
  * a kernel id, each later call records `start` immediately before and `stop`

@@ -110,8 +110,6 @@ __device__ __forceinline__ uint32_t scan_pages(const PoolView &p, int32_t first,
   return found;
 }
 
-__device__ __forceinline__ int32_t pages_of(int64_t rows, int shift) { return (int32_t)((rows + (1 << shift) - 1) >> shift); }
-
 // One workgroup takes a strip of 16 entries of all sessions: it reads them all before it writes any, so the table is
 // permuted in place.  An entry tells by itself whether there is a page behind it, so that no workgroup needs the lengths
 // that another is rewriting.  Counts change by atomics on integers, in any order.
@@ -272,25 +270,7 @@ __global__ __launch_bounds__(kManager) void extend_kernel(PoolView p, const int3
   }
 }
 
-// One workgroup per session gives back the pages behind its new length.
-template <int kThreads>
-__device__ __forceinline__ void trim_session(const PoolView &p, int32_t s, int64_t now, uint32_t *status) {
-  const int64_t was = p.lens[s];
-  if (was < 0 || was > ((int64_t)p.M << p.shift) || now < 0 || now > was) {
-    if (threadIdx.x == 0) raise(status, PLC_ERR_INVALID);
-    return;
-  }
-  for (int32_t j = pages_of(now, p.shift) + (int32_t)threadIdx.x; j < pages_of(was, p.shift); j += kThreads) {
-    int32_t *const entry = &p.table[(int64_t)s * p.M + j];
-    const int32_t page = *entry;
-    *entry = -1;
-    if (p.page_ok(page)) atomicSub(&p.refs[page], 1);
-    else raise(status, PLC_ERR_INVALID);
-  }
-  __syncthreads();  // everybody has read the old length
-  if (threadIdx.x == 0) p.lens[s] = (int32_t)now;
-}
-
+// One workgroup per session.
 __global__ __launch_bounds__(kBlock) void trim_kernel(PoolView p, const int32_t *__restrict__ new_lens, uint32_t *status) {
   trim_session<kBlock>(p, (int32_t)blockIdx.x, new_lens[blockIdx.x], status);
 }
@@ -497,11 +477,6 @@ __global__ __launch_bounds__(kManager) void accept_kernel(PoolView p, const int3
 // Rows between a caller's buffer and pages.  A workgroup takes a block of consecutive rows, as many as give each thread 16
 // bytes of one head, works out where they are, and goes through runs of heads: one, up to the 65,535 that a grid is wide.
 constexpr int kHeadRun = 4;
-struct RowsView {
-  uint16_t *k, *v;
-  int64_t rows, sess_s, layer_s, head_s, row_s;
-  int32_t layer, layers, packed, per_block;
-};
 template <bool kStore, bool kStream>
 __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, const int32_t *__restrict__ off,
                                                       uint32_t *status) {
@@ -511,47 +486,11 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(PoolView p, RowsView r, co
   for (int32_t s = threadIdx.x; s <= p.S; s += kBlock) o[s] = off[s];
   __syncthreads();
   const int64_t x0 = (int64_t)blockIdx.x * r.per_block;
-  if (blockIdx.x == 0 && blockIdx.y == 0) {
-    bool bad = o[0] != 0 || (r.packed && o[p.S] > r.rows);
-    for (int32_t s = threadIdx.x; s < p.S; s += kBlock) bad = bad || o[s + 1] < o[s];
-    if (bad) raise(status, PLC_ERR_INVALID);
-  }
+  if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets<kBlock>(p, r, o, status);
   for (int32_t b = threadIdx.x; b < r.per_block; b += kBlock) {
-    const int64_t x = x0 + b;
-    int64_t pool = -1, buf = 0;
-    int32_t s = 0;
-    int64_t i = 0;
-    bool here;
-    if (r.packed) {
-      int32_t lo = 0, hi = p.S - 1;  // the last session that begins at x or before
-      while (lo < hi) {
-        const int32_t mid = (lo + hi + 1) >> 1;
-        if (o[mid] <= x) lo = mid;
-        else hi = mid - 1;
-      }
-      s = lo;
-      i = x - o[s];
-      here = x < r.rows && i >= 0 && x < o[s + 1];
-      buf = x * r.row_s;
-    } else {
-      s = (int32_t)min(x / r.rows, (int64_t)p.S);
-      i = x - s * r.rows;
-      here = s < p.S && i < (int64_t)o[min(s, p.S - 1) + 1] - o[min(s, p.S - 1)];
-      buf = s * r.sess_s + i * r.row_s;
-    }
-    if (here) {
-      const int64_t t = (int64_t)o[s + 1] - o[s], len = p.lens[s];
-      const int64_t pos = len - t + i;
-      if (t > len || len > ((int64_t)p.M << p.shift) || (!r.packed && t > r.rows)) {
-        raise(status, PLC_ERR_INVALID);
-      } else {
-        const int32_t page = p.table[(int64_t)s * p.M + (pos >> p.shift)];
-        if (p.page_ok(page) && (!kStore || p.refs[page] == 1)) pool = page * p.page_s + (pos & ((1 << p.shift) - 1)) * p.row_s;
-        else raise(status, PLC_ERR_INVALID);
-      }
-    }
-    in_pool[b] = pool;
-    in_buf[b] = buf;
+    const RowPlace at = place_row<kStore>(p, r, o, x0 + b, status);
+    in_pool[b] = at.pool;
+    in_buf[b] = at.buf;
   }
   __syncthreads();
   const int32_t heads = r.layers * p.H, items = r.per_block * p.d8;
@@ -594,21 +533,11 @@ size_t workspace_bytes(const plc_pages *pages) {
 
 int move_rows(bool store, const plc_pages *pages, const plc_rows *rows, const int32_t *off, void *k, void *v,
               uint32_t *status, hipStream_t st) {
-  if (!pages_valid(pages) || !rows || !aligned(off, 4) || !status) return PLC_ERR_INVALID;
-  if (rows->layer < 0 || rows->layers < 1 || rows->layer > pages->L - rows->layers || rows->rows < 0 ||
-      rows->rows > INT32_MAX || (rows->packed != 0 && rows->packed != 1))
-    return PLC_ERR_INVALID;
-  for (int i = 0; i < 4; ++i)
-    if ((i > 0 || !rows->packed) && (rows->stride[i] < 0 || rows->stride[i] % 8)) return PLC_ERR_INVALID;
+  if (!pages_valid(pages) || !rows_valid(pages, rows) || !aligned(off, 4) || !status) return PLC_ERR_INVALID;
   if (rows->rows == 0) return PLC_OK;  // (an empty buffer may have no address)
   if (!aligned(k, 16) || !aligned(v, 16)) return PLC_ERR_INVALID;
   const PoolView p = pool_view(pages);
-  RowsView r;
-  r.k = static_cast<uint16_t *>(k), r.v = static_cast<uint16_t *>(v);
-  r.rows = rows->rows;
-  r.sess_s = rows->stride[0], r.layer_s = rows->stride[1], r.head_s = rows->stride[2], r.row_s = rows->stride[3];
-  r.layer = rows->layer, r.layers = rows->layers, r.packed = rows->packed;
-  r.per_block = p.d8 >= kBlock ? 1 : kBlock / p.d8;
+  const RowsView r = rows_view(rows, k, v, p.d8 >= kBlock ? 1 : kBlock / p.d8);
   const int64_t total = rows->packed ? rows->rows : rows->rows * pages->S;
   const int64_t bx = (total + r.per_block - 1) / r.per_block, heads = (int64_t)r.layers * p.H,
                 by = (heads + kHeadRun - 1) / kHeadRun;

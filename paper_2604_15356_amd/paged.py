@@ -34,6 +34,7 @@ class PagedKVCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.used = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._attend_need = {}
+        self._weights_known = None
         self._attend_ws = [torch.empty(256, dtype=torch.uint8, device=self.device)]
 
     @classmethod
@@ -93,6 +94,19 @@ class PagedKVCache:
         k, v, layer = self._rows(k, v, layer)
         plc.plc_pages_load(self.pages, self._per_session(off, self.S + 1, "off"), k, v, layer, self.status)
 
+    def store_rotated(self, k, v, off, rotary, q=None, base=None, rel=None, layer=0, q_out=None):
+        """`store`, with the keys rotated (rotary.Rotary), and with packed rows the queries q [rows, H*G, d] too: returns them,
+        in q_out, which may be q.  Row i of session s is at position base[s] + rel[row] (int32; default: the positions that the
+        cache has, and i; a tree's nodes: their depths; a cache that was thinned out: what its session has seen)."""
+        k, v, layer = self._rows(k, v, layer)
+        if rotary.d != self.d:
+            raise ValueError(f"a rotation of {rotary.d} components, rows of {self.d}")
+        if q is not None and q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        plc.plc_rotate_store(self.pages, rotary.rotary, self._per_session(off, self.S + 1, "off"), base, rel, k, v, layer, q,
+                             q_out if q is not None else None, self.status)
+        return q_out if q is not None else None
+
     # -- attention ----------------------------------------------------------------------------
     def reserve(self, G, N, max_nodes, max_len=None):
         """Workspace for attend calls of this size, so that none is made during them (under graph capture).  What was
@@ -140,6 +154,48 @@ class PagedKVCache:
         plc.plc_attend(self.pages, layer, q, off, parents, max_nodes, max_len, self.d ** -0.5 if scale is None else scale, out,
                        lse, ws, self.status)
         return out, lse
+
+    # -- what positions have received, and eviction by it ---------------------------------------
+    def make_weights(self):
+        """Zeros for all that positions receive: float32 [S, L, H, positions].  Sessions that are forked take theirs along by
+        weights.copy_(weights[src])."""
+        return torch.zeros((self.S, self.L, self.H, self.M * self.B), dtype=torch.float32, device=self.device)
+
+    def _weights(self, w):
+        layout = w.shape, w.stride(), w.dtype, w.device
+        if self._weights_known is None or self._weights_known[0] != layout:
+            if w.device != self.device:
+                raise ValueError("the weights are on another device than the cache")
+            self._weights_known = layout, plc.make_weights(self.pages, w)
+        view = self._weights_known[1]
+        view.w = w.data_ptr()
+        return view
+
+    def add_weights(self, q, off, lse, weights, decay=1.0, layer=0, scale=None, max_nodes=None, max_len=None):
+        """Adds to weights (make_weights) what `layer`'s positions receive from the sessions' last off[s+1] - off[s] positions, a
+        chain: q [N, H*G, d] and lse [N, H*G] as for attend and from it, so many times what was there before (`decay`; the call's own
+        positions begin with nothing).  Of a drafted tree only what was accepted counts: call it after `accept`, with those rows."""
+        if q.dim() != 3 or q.dtype is not self.dtype:
+            raise ValueError(f"q is [nodes, heads, d] of {self.dtype}")
+        N = q.shape[0]
+        self._per_session(off, self.S + 1, "off")
+        view = self._weights(weights)
+        if N == 0:
+            return
+        plc.plc_attend_weights(self.pages, layer, q, off, N if max_nodes is None else max_nodes,
+                               self.M * self.B if max_len is None else max_len, self.d ** -0.5 if scale is None else scale, lse,
+                               decay, view, self.status)
+
+    def evict(self, keep, weights, kept=None, first=0, last=0, max_len=None):
+        """Every session of more than keep[s] positions (int32 [S]) is shortened to that, in each layer and head to its first and
+        last positions and those with the largest weights, which move along.  Returns kept, int32 [S, L, H, W]: the positions
+        that stayed, in front; given, its W bounds keep and shorter sessions.  The pages from position `first` on have to be the sessions' own."""
+        self._per_session(keep, self.S, "keep")
+        max_len = self.M * self.B if max_len is None else max_len
+        if kept is None:
+            kept = torch.empty((self.S, self.L, self.H, max_len), dtype=torch.int32, device=self.device)
+        plc.plc_pages_evict(self.pages, keep, first, last, self._weights(weights), kept, max_len, self.ws, self.status)
+        return kept
 
     def check_status(self, where="plc_pages"):
         """Synchronises and raises if a kernel reported a data-dependent error."""

@@ -37,11 +37,15 @@ EXPORTS = ("plc_version", "plc_strerror", "plc_workspace_bytes", "plc_units_per_
            "plc_expected_embedding", "plc_predict_residual_linear", "plc_reconstruct_linear",
            "plc_pages_workspace_bytes", "plc_pages_fork", "plc_pages_extend", "plc_pages_trim", "plc_pages_accept",
            "plc_pages_compact", "plc_pages_store", "plc_pages_load", "plc_attend_workspace_bytes", "plc_attend",
+           "plc_rotary_frequencies", "plc_rotary_turns", "plc_rotate", "plc_rotate_store", "plc_attend_weights", "plc_pages_evict",
+           "plc_score_workspace_bytes", "plc_score_tokens",
            "plc_trie_create", "plc_trie_destroy", "plc_trie_size", "plc_trie_nodes", "plc_trie_insert",
            "plc_trie_best_match", "plc_trie_evict")
 
 MAX_BITS = 4
-PLC_FP16, PLC_BF16 = 0, 1
+PLC_FP16, PLC_BF16, PLC_FP32 = 0, 1, 2
+ROTARY_SCALINGS = ("none", "linear", "stretched", "parts", "ramp")  # PLC_ROTARY_*
+MOST_ALTERNATIVES = 32
 TREE_NODES = 256
 RESTART_WORDS = 34
 
@@ -77,6 +81,19 @@ class plc_pages(C.Structure):
 class plc_rows(C.Structure):
     _fields_ = [("layer", C.c_int32), ("layers", C.c_int32), ("packed", C.c_int32), ("rows", C.c_int64),
                 ("stride", C.c_int64 * 4)]
+
+
+class plc_rotary_spec(C.Structure):
+    _fields_ = [("r", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("trained", C.c_int64)]
+
+
+class plc_rotary(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("r", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
+
+
+class plc_weights(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("stride", C.c_int64 * 3), ("width", C.c_int64)]
 
 
 _lib = None
@@ -158,6 +175,16 @@ def lib() -> C.CDLL:
         L.plc_attend_workspace_bytes.restype = sz
         L.plc_attend_workspace_bytes.argtypes = [gp, i32, i64, i32, i32]
         L.plc_attend.argtypes = [gp, i32, i32, p, i64s, i32, i64, p, p, i32, i32, C.c_float, p, i64s, p, p, sz, p, p]
+        yp, wp, f32 = C.POINTER(plc_rotary), C.POINTER(plc_weights), C.c_float
+        L.plc_rotary_frequencies.argtypes = [C.POINTER(plc_rotary_spec), p]
+        L.plc_rotary_turns.argtypes = [p, i32, p]
+        L.plc_rotate.argtypes = [yp, i32, p, i64s, i64, i32, i32, p, i32, p, i64s, p]
+        L.plc_rotate_store.argtypes = [gp, kp, yp, i32, p, p, p, p, p, p, i64s, i32, p, i64s, p, p]
+        L.plc_attend_weights.argtypes = [gp, i32, i32, p, i64s, i32, i64, p, i32, i32, f32, p, f32, wp, p, p]
+        L.plc_pages_evict.argtypes = [gp, p, i32, i32, wp, p, i32, i32, p, sz, p, p]
+        L.plc_score_workspace_bytes.restype = sz
+        L.plc_score_workspace_bytes.argtypes = [i32, i32]
+        L.plc_score_tokens.argtypes = [i32, p, i64, i64, i32, f32, p, i32, p, p, p, p, p, p, p, p, sz, p, p]
         L.plc_trie_create.restype = p
         L.plc_trie_create.argtypes = [C.c_double]
         L.plc_trie_destroy.restype = None
@@ -666,6 +693,156 @@ def plc_attend(pages, layer, q, off, parents, max_nodes, max_len, scale, out, ls
                             max_len, scale, out.data_ptr(), q_stride if os_ == qs else _I64x2(os_[0], os_[1]),
                             None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _ints(status),
                             _stream_of(q)), "plc_attend")
+
+
+# ---- rotary positions, weights of positions, scores of tokens ------------------------------------------------------------
+
+def plc_rotary_frequencies(r, scaling="none", base=10000.0, factor=1.0, low=1.0, high=2.0, trained=1):
+    """Radians a position of each of r / 2 pairs: a list.  Host call."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling is one of {', '.join(ROTARY_SCALINGS)}")
+    theta = (C.c_double * max(int(r) // 2, 1))()
+    spec = plc_rotary_spec(r, ROTARY_SCALINGS.index(scaling), base, factor, low, high, trained)
+    _check(lib().plc_rotary_frequencies(spec, theta), "plc_rotary_frequencies")
+    return list(theta)
+
+
+def plc_rotary_turns(theta):
+    """theta: radians a position, any numbers.  Their turns, in 2^-64: a list of whole numbers.  Host call."""
+    theta = (C.c_double * len(theta))(*theta)
+    turns = (C.c_uint64 * len(theta))()
+    _check(lib().plc_rotary_turns(theta, len(theta), turns), "plc_rotary_turns")
+    return list(turns)
+
+
+def make_rotary(turns, interleaved, magnitude) -> plc_rotary:
+    """turns: int64 [r / 2], the bits of plc_rotary_turns; it has to outlive what is made here."""
+    return plc_rotary(_contig(turns, torch.int64), 2 * turns.numel(), 1 if interleaved else 0, magnitude)
+
+
+def _on(device, *tensors):
+    """All of them (None aside) on the device that launches go to."""
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"plc works on the current device, {device}; a tensor is on {t.device}")
+
+
+def _floats(t):
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or not t.is_contiguous():
+        raise TypeError("expected contiguous float32")
+    return t.data_ptr()
+
+
+def _ints_or_none(t):
+    return None if t is None else _ints(t)
+
+
+def _type16(t):
+    if t.dtype is torch.float16:
+        return PLC_FP16
+    if t.dtype is torch.bfloat16:
+        return PLC_BF16
+    raise TypeError(f"expected float16 or bfloat16, got {t.dtype}")
+
+
+def _rows_in_and_out(x, out):
+    """[rows, heads, d] twice, of one type and shape: the strides of row and head of each."""
+    shape, xs, os_ = x.shape, x.stride(), out.stride()
+    if len(shape) != 3 or shape != out.shape or x.dtype is not out.dtype or xs[2] != 1 or os_[2] != 1:
+        raise ValueError("rows in and out are [rows, heads, d] of one type, with contiguous components")
+    return _I64x2(xs[0], xs[1]), _I64x2(os_[0], os_[1])
+
+
+def plc_rotate(rotary, x, positions, inverse, out):
+    """x, out [rows, heads, d], components contiguous; positions int32 [rows].  out may be x."""
+    stream = _stream_of(x)
+    _on(x.get_device(), positions, out)
+    x_stride, out_stride = _rows_in_and_out(x, out)
+    if positions.dim() != 1 or positions.shape[0] != x.shape[0]:
+        raise ValueError("positions are int32 [rows]")
+    _check(lib().plc_rotate(rotary, _type16(x), x.data_ptr(), x_stride, x.shape[0], x.shape[1], x.shape[2], _ints(positions),
+                            1 if inverse else 0, out.data_ptr(), out_stride, stream), "plc_rotate")
+
+
+def plc_rotate_store(pages, rotary, off, base, rel, k, v, layer, q, q_out, status):
+    """k, v as for plc_pages_store; base int32 [S] or None; rel int32, one for each row of k (packed [rows], else [S, rows]), or
+    None; q, q_out [rows, H*G, d] or None (packed rows only)."""
+    stream = _stream_of(off)
+    _on(off.get_device(), base, rel, k, v, q, q_out, status)
+    rows = _rows_of(pages, k, v, layer)
+    if base is not None and (base.dim() != 1 or base.shape[0] != pages.S):
+        raise ValueError("base is int32 [sessions]")
+    if rel is not None and tuple(rel.shape) != ((k.shape[0],) if rows.packed else (k.shape[0], k.shape[3])):
+        raise ValueError("rel has a number for each row")
+    q_stride = out_stride = None
+    G = 1
+    if q is not None:
+        q_stride, out_stride = _rows_in_and_out(q, q_out)
+        if q.dtype is not k.dtype or q.shape[0] != k.shape[0] or q.shape[1] % pages.H or q.shape[2] != pages.d or not rows.packed:
+            raise ValueError("q is [rows, heads, d], packed like k and of its type, its heads a multiple of the cache's")
+        G = q.shape[1] // pages.H
+    _check(lib().plc_rotate_store(pages, rows, rotary, _type16(k), _ints(off), _ints_or_none(base), _ints_or_none(rel), k.data_ptr(),
+                                  v.data_ptr(), None if q is None else q.data_ptr(), q_stride, G,
+                                  None if q is None else q_out.data_ptr(), out_stride, _ints(status), stream), "plc_rotate_store")
+
+
+def make_weights(pages, w) -> plc_weights:
+    """w float32 [S, L, H, width]; it has to outlive what is made here."""
+    if w.dim() != 4 or w.dtype is not torch.float32 or tuple(w.shape[:3]) != (pages.S, pages.L, pages.H) or w.stride(3) != 1:
+        raise ValueError("weights are float32 [sessions, layers, heads, positions] of the cache, positions contiguous")
+    return plc_weights(_ptr(w, torch.float32), w.stride()[:3], w.shape[3])
+
+
+def plc_attend_weights(pages, layer, q, off, max_nodes, max_len, scale, lse, decay, weights, status):
+    """q [N, H*G, d], components contiguous; lse float32 [N, H*G]; weights: make_weights."""
+    stream = _stream_of(q)
+    _on(q.get_device(), off, lse, status)
+    shape, qs = q.shape, q.stride()
+    if len(shape) != 3 or qs[2] != 1 or shape[1] % pages.H or shape[2] != pages.d:
+        raise ValueError("q is [nodes, heads, d], its heads a multiple of the cache's, with contiguous components")
+    if lse.shape != shape[:2]:
+        raise ValueError("lse is [nodes, heads]")
+    _check(lib().plc_attend_weights(pages, layer, _type16(q), q.data_ptr(), _I64x2(qs[0], qs[1]), shape[1] // pages.H, shape[0],
+                                    _ints(off), max_nodes, max_len, scale, _floats(lse), decay, weights, _ints(status), stream),
+           "plc_attend_weights")
+
+
+def plc_pages_evict(pages, keep, first, last, weights, kept, max_len, ws, status):
+    """keep int32 [S]; weights: make_weights; kept int32 [S, L, H, W] out."""
+    stream = _stream_of(keep)
+    _on(keep.get_device(), kept, ws, status)
+    if kept.dim() != 4 or tuple(kept.shape[:3]) != (pages.S, pages.L, pages.H):
+        raise ValueError("kept is int32 [sessions, layers, heads, numbers]")
+    _check(lib().plc_pages_evict(pages, _ints(keep), first, last, weights, _ints(kept), kept.shape[3], max_len, _on_device(ws),
+                                 ws.numel(), _ints(status), stream), "plc_pages_evict")
+
+
+def plc_score_workspace_bytes(V, k) -> int:
+    return int(lib().plc_score_workspace_bytes(V, k))
+
+
+_LOGIT_TYPES = {torch.float16: PLC_FP16, torch.bfloat16: PLC_BF16, torch.float32: PLC_FP32}
+
+
+def plc_score_tokens(logits, scale, tokens, k, logprob, entropy, lse, ids, top_logprobs, probs, chosen, ws, status):
+    """logits [N, V], the tokens contiguous; tokens int32 [N] or None; out, or None: logprob, entropy, lse float32 [N], ids int32 and
+    top_logprobs, probs float32 [N, k], chosen int32 [N]."""
+    stream = _stream_of(logits)
+    _on(logits.get_device(), tokens, logprob, entropy, lse, ids, top_logprobs, probs, chosen, ws, status)
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits are [rows, tokens], the tokens contiguous")
+    if logits.dtype not in _LOGIT_TYPES:
+        raise TypeError(f"expected float16, bfloat16 or float32, got {logits.dtype}")
+    N, V = logits.shape
+    for t, n in ((tokens, N), (logprob, N), (entropy, N), (lse, N), (chosen, N), (ids, N * k), (top_logprobs, N * k), (probs, N * k)):
+        if t is not None and t.numel() != n:
+            raise ValueError("a result or the tokens do not have a place for each row (and alternative)")
+    _check(lib().plc_score_tokens(_LOGIT_TYPES[logits.dtype], logits.data_ptr(), logits.stride(0), N, V, scale, _ints_or_none(tokens),
+                                  k, _floats(logprob), _floats(entropy), _floats(lse), _ints_or_none(ids), _floats(top_logprobs),
+                                  _floats(probs), _ints_or_none(chosen), _on_device(ws), ws.numel(), _ints(status), stream),
+           "plc_score_tokens")
 
 
 class PrefixTrie:
