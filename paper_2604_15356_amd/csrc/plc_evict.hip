@@ -170,28 +170,46 @@ __global__ __launch_bounds__(kBlock) void move_kernel(EvictArgs a) {
   const int32_t column = unit % a.columns, of_v = unit / a.columns & 1, lh = unit / (2 * a.columns);
   const int32_t at_once = kBlock / a.pieces, row = (int32_t)threadIdx.x / a.pieces, c = column * a.pieces + (int32_t)threadIdx.x % a.pieces;
   const bool here = row < at_once && c < p.d8;
-  uint16_t *const base = (of_v ? p.v : p.k) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)c * 8;
+  uint16_t *const base = (of_v ? p.v : p.k) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)min(c, p.d8 - 1) * 8;
   const int32_t *const kept = a.kept + ((int64_t)s * heads + lh) * a.W, *const table = p.table + (int64_t)s * p.M;
   const int32_t mask = (1 << p.shift) - 1;
-  for (int32_t j0 = a.first; j0 < now; j0 += kMoveBatch * at_once) {
+  const int32_t round = kMoveBatch * at_once, last = now - 1;
+  int32_t from[kMoveBatch], from_page[kMoveBatch], to_page[kMoveBatch];
+  const auto fetch = [&](int32_t j0) {  // (rows behind the end are read as the last one, and not written)
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) from[u] = kept[min(j0 + u * at_once + row, last)];
+  };
+  const auto fetch_pages = [&](int32_t j0) {
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) {
+      from_page[u] = table[from[u] >> p.shift];
+      to_page[u] = table[min(j0 + u * at_once + row, last) >> p.shift];
+    }
+  };
+  int32_t j0 = a.first;
+  while (j0 + round <= now && kept[j0 + round - 1] == j0 + round - 1) j0 += round;  // nothing has gone before these
+  if (j0 >= now) return;
+  fetch(j0);
+  fetch_pages(j0);
+  for (; j0 < now; j0 += round) {
     uint4 v[kMoveBatch];
-    int32_t to[kMoveBatch];
+    uint16_t *to[kMoveBatch];
+    bool moves[kMoveBatch];
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
       const int32_t j = j0 + u * at_once + row;
-      to[u] = -1;
-      if (here && j < now) {
-        const int32_t from = kept[j];
-        if (from != j) {
-          to[u] = j;
-          v[u] = *reinterpret_cast<const uint4 *>(base + table[from >> p.shift] * p.page_s + (from & mask) * p.row_s);
-        }
-      }
+      v[u] = *reinterpret_cast<const uint4 *>(base + from_page[u] * p.page_s + (from[u] & mask) * p.row_s);
+      to[u] = base + to_page[u] * p.page_s + (j & mask) * p.row_s;
+      moves[u] = here && j < now && from[u] != j;
+    }
+    if (j0 + round < now) {
+      fetch(j0 + round);
+      fetch_pages(j0 + round);
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u)
-      if (to[u] >= 0) *reinterpret_cast<uint4 *>(base + table[to[u] >> p.shift] * p.page_s + (to[u] & mask) * p.row_s) = v[u];
+      if (moves[u]) *reinterpret_cast<uint4 *>(to[u]) = v[u];
   }
 }
 
