@@ -35,38 +35,52 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 }
 
 constexpr int kBins = 2048;
+// A bin's place: the wavefront that adds them up, 32 in a row to a lane, so reads from all banks.
+__device__ __forceinline__ uint32_t place_of(uint32_t bin) { return (bin & (kBins / 64 - 1)) * 64 + bin / (kBins / 64); }
+constexpr int64_t kCached = (int64_t)96 << 20;  // bytes moved, in and out, beyond which rows go past the caches
 
-// Exclusive prefix sum over a workgroup.  `smem`: a word for each wavefront and one more.
+// Runs of four positions that a thread holds, at a distance of the workgroup's: 16 positions for each thread are looked at without
+// being read again.
+constexpr int kRuns = 4;
 template <int kThreads>
-__device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t *smem, uint32_t *total) {
-  constexpr int kWaves = kThreads / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t inc = wave_inclusive_scan(v);
-  __syncthreads();
-  if (lane == 63) smem[wave] = inc;
-  __syncthreads();
-  uint32_t base = 0, all = 0;
+struct Held {
+  static constexpr int32_t kRound = 4 * kThreads, kAll = kRuns * kRound;
+  uint32_t key[kRuns][4];
+  float w[kRuns][4];
+  __device__ __forceinline__ void load(const float *weights, int32_t i0, int32_t n) {
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const uint32_t s = smem[w];
-    base += w < wave ? s : 0;
-    all += s;
+    for (int c = 0; c < kRuns; ++c) {
+      const int32_t i = i0 + c * kRound + 4 * (int32_t)threadIdx.x;
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (i < n) v = *reinterpret_cast<const float4 *>(weights + i);  // (a width's last run is whole: checked on the host)
+      w[c][0] = v.x, w[c][1] = v.y, w[c][2] = v.z, w[c][3] = v.w;
+    }
+#pragma unroll
+    for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) key[c][e] = key_of(w[c][e]);
   }
-  *total = all;
-  return base + inc - v;
-}
+};
 
 template <int kThreads>
 __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
-  __shared__ uint32_t bins[kBins];
-  __shared__ uint32_t smem[kThreads / 64 + 1];
-  __shared__ uint32_t found[2];
+  constexpr int kWaves = kThreads / 64;
+  using Block = Held<kThreads>;
+  __shared__ __attribute__((aligned(16))) uint32_t bins[2][kBins];
+  __shared__ uint32_t meet[kRuns][kWaves];
+  __shared__ uint32_t found[3];
   const PoolView &p = a.p;
   const int32_t s = (int32_t)blockIdx.y, lh = (int32_t)blockIdx.x, heads = p.L * p.H;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t len = p.lens[s], keep = a.keep[s], now = min(len, keep);
   bool ok = len >= 0 && len <= a.max_len && len <= ((int64_t)p.M << p.shift) && len <= a.w.width && keep >= 0 && now <= a.W &&
             (now == len || now >= (int64_t)a.first + a.last);
-  if (ok && now < len) {
+  float *const w = a.w.w + s * a.w.sess_s + (lh / p.H) * a.w.layer_s + (lh % p.H) * a.w.head_s;
+  const bool shorter = ok && now < len;
+  Block held;
+  if (shorter) held.load(w, 0, (int32_t)len);
+  for (int i = 4 * threadIdx.x; i < kBins; i += 4 * kThreads) *reinterpret_cast<uint4 *>(&bins[0][i]) = make_uint4(0u, 0u, 0u, 0u);
+  if (shorter) {
     // the pages in use, and those that are written among them
     for (int32_t j = threadIdx.x; j < pages_of(len, p.shift); j += kThreads) {
       const int32_t page = p.table[(int64_t)s * p.M + j];
@@ -85,83 +99,113 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
     for (int32_t j = threadIdx.x; j < now; j += kThreads) kept[j] = j;
     return;
   }
-  float *const w = a.w.w + s * a.w.sess_s + (lh / p.H) * a.w.layer_s + (lh % p.H) * a.w.head_s;
   const int32_t n = (int32_t)len, lo = a.first, hi = n - a.last;  // positions lo .. hi-1 are chosen from
   uint32_t want = (uint32_t)now - (uint32_t)(a.first + a.last);   // of them stay (fewer than there are)
+  const bool some = want > 0;                                     // else nobody but the first and the last
 
   // The key of the last one that stays, digit by digit: of the keys that begin as it does, `want` are still to be found.
   uint32_t prefix = 0;
 #pragma unroll 1
-  for (int digit = 0; digit < 3 && want > 0; ++digit) {
+  for (int digit = 0; digit < 3 && some; ++digit) {
     const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
-    __syncthreads();
-    for (int32_t i = (lo & ~3) + 4 * (int32_t)threadIdx.x; i < hi; i += 4 * kThreads) {
-      const float4 v = *reinterpret_cast<const float4 *>(w + i);  // (a width's last piece is whole: checked on the host)
+    uint32_t *const count = bins[digit & 1];
+    for (int32_t i0 = 0; i0 < hi; i0 += Block::kAll) {
+      if (n > Block::kAll) held.load(w, i0, n);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t key = key_of(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
-        if (i + e >= lo && i + e < hi && (digit == 0 || key >> (shift + bits) == prefix))
-          atomicAdd(&bins[key >> shift & ((1u << bits) - 1)], 1u);
+      for (int c = 0; c < kRuns; ++c) {
+        if (i0 + c * Block::kRound >= hi) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int32_t i = i0 + c * Block::kRound + 4 * (int32_t)threadIdx.x + e;
+          const uint32_t key = held.key[c][e];
+          if (i >= lo && i < hi && (digit == 0 || key >> (shift + bits) == prefix)) atomicAdd(&count[place_of(key >> shift & ((1u << bits) - 1))], 1u);
+        }
       }
     }
     __syncthreads();
-    // the digits from the largest down: the first behind which there are `want`
-    constexpr int kEach = kBins / kThreads;
-    uint32_t mine = 0;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) mine += bins[kBins - 1 - (kEach * (int)threadIdx.x + e)];
-    uint32_t total, before = scan<kThreads>(mine, smem, &total);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int bin = kBins - 1 - (kEach * (int)threadIdx.x + e);
-      if (before < want && before + bins[bin] >= want) found[0] = (uint32_t)bin, found[1] = want - before;
-      before += bins[bin];
+    if (wave == 0) {  // the digits from the largest down, 32 to a lane: the one behind which there are `want`
+      uint32_t mine = 0;
+#pragma unroll 8
+      for (int e = 0; e < kBins / 64; ++e) mine += count[e * 64 + 63 - lane];
+      uint32_t upto = wave_inclusive_scan(mine);
+      const int owner = __builtin_ctzll(__ballot(upto >= want));  // (all of them are more)
+      uint32_t before = owner > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)upto, owner - 1) : 0u;
+      const uint32_t one = lane < kBins / 64 ? count[(kBins / 64 - 1 - lane) * 64 + 63 - owner] : 0u;
+      upto = before + wave_inclusive_scan(one);
+      const int nth = __builtin_ctzll(__ballot(upto >= want));
+      if (nth > 0) before = (uint32_t)__builtin_amdgcn_readlane((int)upto, nth - 1);
+      const uint32_t with = (uint32_t)__builtin_amdgcn_readlane((int)upto, nth);
+      if (lane == 0) found[0] = (uint32_t)(kBins - 1 - owner * (kBins / 64) - nth), found[1] = want - before, found[2] = with == want;
+    } else if (digit < 2) {  // the next digit's
+      for (int i = 4 * (threadIdx.x - 64); i < kBins; i += 4 * (kThreads - 64))
+        *reinterpret_cast<uint4 *>(&bins[(digit & 1) ^ 1][i]) = make_uint4(0u, 0u, 0u, 0u);
     }
     __syncthreads();
     prefix = prefix << bits | found[0];
     want = found[1];
-    __syncthreads();
+    if (found[2]) {  // all that begin so stay: what follows does not matter
+      prefix = (prefix << shift) - 1;  // (not of zero: then all positions would stay)
+      want = 0;
+      break;
+    }
   }
-  const bool some = now > (int64_t)a.first + a.last;  // else nobody but the first and the last
   // Keys above `prefix` stay, and of those equal to it the first `want`.
   uint32_t above = 0, equal = 0;  // so far
-  for (int32_t i0 = 0; i0 < n; i0 += 4 * kThreads) {
-    const int32_t i = i0 + 4 * (int32_t)threadIdx.x;
-    float v[4] = {};
-    uint32_t up = 0, same = 0;
-    if (i < n) {
-      const float4 x = *reinterpret_cast<const float4 *>(w + i);
-      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+  for (int32_t i0 = 0; i0 < n; i0 += Block::kAll) {
+    if (n > Block::kAll) held.load(w, i0, n);
+    uint32_t up[kRuns], same[kRuns], counts[kRuns], upto[kRuns];
+#pragma unroll
+    for (int c = 0; c < kRuns; ++c) {
+      if (i0 + c * Block::kRound >= n) break;
+      up[c] = same[c] = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t key = key_of(v[e]);
-        const bool mid = i + e >= lo && i + e < hi, in = i + e < n;
-        up |= (uint32_t)(in && (!mid || (some && key > prefix))) << e;
-        same |= (uint32_t)(in && mid && some && key == prefix) << e;
+        const int32_t i = i0 + c * Block::kRound + 4 * (int32_t)threadIdx.x + e;
+        const uint32_t key = held.key[c][e];
+        const bool mid = i >= lo && i < hi;
+        up[c] |= (uint32_t)(i < n && (!mid || (some && key > prefix))) << e;
+        same[c] |= (uint32_t)(mid && some && key == prefix) << e;
       }
+      counts[c] = (uint32_t)__builtin_popcount(up[c]) | (uint32_t)__builtin_popcount(same[c]) << 16;
+      upto[c] = wave_inclusive_scan(counts[c]);
+      if (lane == 63) meet[c][wave] = upto[c];
     }
-    uint32_t total;
-    const uint32_t before = scan<kThreads>((uint32_t)__builtin_popcount(up) | (uint32_t)__builtin_popcount(same) << 16, smem, &total);
-    uint32_t g = above + (before & 0xffffu), q = equal + (before >> 16);
-    // (everybody has read the weights of this round: what is written lies at or before them)
+    __syncthreads();
+    // (everybody has read the weights of these runs: what is written lies at or before them)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool is_same = same >> e & 1u, stays = (up >> e & 1u) || (is_same && q < want);
-      if (stays) {
-        const uint32_t j = g + min(q, want);
-        kept[j] = i + e;
-        if ((int32_t)j != i + e) w[j] = v[e];
+    for (int c = 0; c < kRuns; ++c) {
+      if (i0 + c * Block::kRound >= n) break;
+      uint32_t before = 0, total = 0;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        const uint32_t x = meet[c][v];
+        before += v < wave ? x : 0;
+        total += x;
       }
-      g += up >> e & 1u;
-      q += is_same;
+      before += upto[c] - counts[c];
+      uint32_t g = above + (before & 0xffffu), q = equal + (before >> 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int32_t i = i0 + c * Block::kRound + 4 * (int32_t)threadIdx.x + e;
+        const bool is_same = same[c] >> e & 1u;
+        if ((up[c] >> e & 1u) || (is_same && q < want)) {
+          const uint32_t j = g + min(q, want);
+          kept[j] = i;
+          if ((int32_t)j != i) w[j] = held.w[c][e];
+        }
+        g += up[c] >> e & 1u;
+        q += is_same;
+      }
+      above += total & 0xffffu, equal += total >> 16;
     }
-    above += total & 0xffffu, equal += total >> 16;
+    __syncthreads();  // `meet` is written again
   }
 }
 
-// A lane takes 16 bytes of a row, several rows at a time; all of the workgroup's loads of a round before its first store.
+// A lane takes 16 bytes of a row, several rows at a time; all of the workgroup's loads of a round before its first store, and the next
+// round's addresses while they are under way.  kStream: past the caches, in and out.
 constexpr int kMoveBatch = 8;
+template <bool kStream>
 __global__ __launch_bounds__(kBlock) void move_kernel(EvictArgs a) {
   const PoolView &p = a.p;
   const int32_t s = (int32_t)blockIdx.y, now = a.now[s];
@@ -172,16 +216,16 @@ __global__ __launch_bounds__(kBlock) void move_kernel(EvictArgs a) {
   const bool here = row < at_once && c < p.d8;
   uint16_t *const base = (of_v ? p.v : p.k) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)min(c, p.d8 - 1) * 8;
   const int32_t *const kept = a.kept + ((int64_t)s * heads + lh) * a.W, *const table = p.table + (int64_t)s * p.M;
-  const int32_t mask = (1 << p.shift) - 1;
-  const int32_t round = kMoveBatch * at_once, last = now - 1;
-  int32_t from[kMoveBatch], from_page[kMoveBatch], to_page[kMoveBatch];
+  const int32_t mask = (1 << p.shift) - 1, round = kMoveBatch * at_once, last = now - 1;
+  int32_t from[kMoveBatch], next[kMoveBatch], from_page[kMoveBatch], to_page[kMoveBatch];
   const auto fetch = [&](int32_t j0) {  // (rows behind the end are read as the last one, and not written)
 #pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u) from[u] = kept[min(j0 + u * at_once + row, last)];
+    for (int u = 0; u < kMoveBatch; ++u) next[u] = kept[min(j0 + u * at_once + row, last)];
   };
   const auto fetch_pages = [&](int32_t j0) {
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
+      from[u] = next[u];
       from_page[u] = table[from[u] >> p.shift];
       to_page[u] = table[min(j0 + u * at_once + row, last) >> p.shift];
     }
@@ -192,24 +236,26 @@ __global__ __launch_bounds__(kBlock) void move_kernel(EvictArgs a) {
   fetch(j0);
   fetch_pages(j0);
   for (; j0 < now; j0 += round) {
-    uint4 v[kMoveBatch];
+    u32x4 v[kMoveBatch];
     uint16_t *to[kMoveBatch];
     bool moves[kMoveBatch];
+    if (j0 + round < now) fetch(j0 + round);
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
       const int32_t j = j0 + u * at_once + row;
-      v[u] = *reinterpret_cast<const uint4 *>(base + from_page[u] * p.page_s + (from[u] & mask) * p.row_s);
+      const auto *const at = reinterpret_cast<const u32x4 *>(base + from_page[u] * p.page_s + (from[u] & mask) * p.row_s);
+      v[u] = kStream ? __builtin_nontemporal_load(at) : *at;
       to[u] = base + to_page[u] * p.page_s + (j & mask) * p.row_s;
       moves[u] = here && j < now && from[u] != j;
     }
-    if (j0 + round < now) {
-      fetch(j0 + round);
-      fetch_pages(j0 + round);
-    }
+    if (j0 + round < now) fetch_pages(j0 + round);
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u)
-      if (moves[u]) *reinterpret_cast<uint4 *>(to[u]) = v[u];
+      if (moves[u]) {
+        if (kStream) __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4 *>(to[u]));
+        else *reinterpret_cast<u32x4 *>(to[u]) = v[u];
+      }
   }
 }
 
@@ -235,16 +281,20 @@ extern "C" int plc_pages_evict(const plc_pages *pages, const int32_t *keep, int3
   a.w = weights_view(weights);
   a.keep = keep, a.kept = kept, a.now = static_cast<int32_t *>(ws);
   a.first = first, a.last = last, a.W = W, a.max_len = max_len;
-  a.pieces = a.p.d8 % 8 == 0 ? 8 : a.p.d8 < kBlock ? a.p.d8 : kBlock;
-  a.columns = (a.p.d8 + a.pieces - 1) / a.pieces;
   a.status = status;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t heads = (int64_t)a.p.L * a.p.H;
   if (heads >= 1 << 22 || heads * pages->d >= 1 << 29) return PLC_ERR_INVALID;  // (lanes of a launch < 2^32)
   const dim3 grid((unsigned)heads, (unsigned)a.p.S);
+  // Whole rows where there are heads enough to fill the chip (4 sessions, 32 layers, 8 heads, 2048 positions to half: 244 against 250 us; 64
+  // sessions of 200: 452 against 474), else lines of 128 bytes, a workgroup each.
+  const int64_t rows = heads * a.p.S;
+  a.pieces = a.p.d8 > kBlock ? kBlock : a.p.d8 % 16 == 0 && rows >= 2 * kComputeUnits ? 16 : a.p.d8 % 8 == 0 ? 8 : a.p.d8;
+  a.columns = (a.p.d8 + a.pieces - 1) / a.pieces;
+  const bool past = (double)rows * W * a.p.d8 * 64 > (double)kCached;  // of both halves, in and out
   if (max_len <= 4096) hipLaunchKernelGGL(select_kernel<256>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(select_kernel<1024>, grid, dim3(1024), 0, st, a);
-  hipLaunchKernelGGL(move_kernel, dim3((unsigned)(heads * 2 * a.columns), (unsigned)a.p.S), dim3(kBlock), 0, st, a);
+  hipLaunchKernelGGL(past ? &move_kernel<true> : &move_kernel<false>, dim3((unsigned)(heads * 2 * a.columns), (unsigned)a.p.S), dim3(kBlock), 0, st, a);
   hipLaunchKernelGGL(shorten_kernel, dim3((unsigned)a.p.S), dim3(kBlock), 0, st, a);
   return launch_status();
 }

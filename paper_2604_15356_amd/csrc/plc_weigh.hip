@@ -6,6 +6,7 @@
 // so that a lane's 16 accumulators are rows of one position: their weights exp2(scale' S - lse') are added up in the lane itself,
 // row by row in a fixed order, and only the two halves of a position meet at the end.  K is read once, straight into the operand's
 // registers (a lane holds 16 bytes of its position's row at a time); nothing of the scores leaves the registers.
+#include <atomic>
 #include <type_traits>
 
 #include "plc_device.h"
@@ -19,8 +20,11 @@ typedef short short8v __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) float lds_float;
+typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kSpanOfGroup = 32 * (kBlock / 64);  // positions of a workgroup, 32 of each wavefront
 constexpr int64_t kMostGroups = 1 << 16;  // workgroups: bounds from the host may be far above what there is to do
 
 struct WeighArgs {
@@ -61,6 +65,17 @@ __device__ __forceinline__ SessionView session_of(const WeighArgs &a, int s, boo
 
 __device__ __forceinline__ void put_weight(const WeighArgs &a, float *at, bool old, float before, float sum) {
   *at = old && a.decay != 0.0f ? __builtin_fmaf(a.decay, before, sum) : sum;
+}
+
+// LDS layout of a stage of rows: rows of DP components; the 16-byte piece c of row r stands in place c ^ turn(r), so that 16 consecutive
+// rows' same piece spread over all banks.
+template <int DP>
+__device__ __forceinline__ int turn(int r) {
+  return DP == 64 ? r >> 1 & 7 : r & 15;
+}
+template <int DP>
+__device__ __forceinline__ int place(int r, int c) {
+  return r * (DP * 2) + ((c ^ turn<DP>(r)) << 4);
 }
 
 // Up to 32 rows: they stay in registers, and the positions stream by, kTiles times 32 for each wavefront, the next ones' rows of K on their way
@@ -146,32 +161,32 @@ __global__ __launch_bounds__(kBlock, DP <= 128 ? 2 : 1) void weigh_few_kernel(We
   }
 }
 
-// LDS layout of a stage: kStageRows rows of DP components; the 16-byte piece c of row r stands in place c ^ turn(r), so that 16
-// consecutive rows' same piece spread over all banks.
-constexpr int kStageRows = 64;
-template <int DP>
-__device__ __forceinline__ int turn(int r) {
-  return DP == 64 ? r >> 1 & 7 : r & 15;
-}
-template <int DP>
-__device__ __forceinline__ int place(int r, int c) {
-  return r * (DP * 2) + ((c ^ turn<DP>(r)) << 4);
-}
+// More rows: four wavefronts keep 32 positions each in registers, and the rows come by in stages of 64 that they share, the next one on
+// its way to LDS while one is worked on.
+template <int DP_>
+struct ManyShape {
+  static constexpr int DP = DP_, kRows = 64, kSpan = kSpanOfGroup;
+  static constexpr int kStage = kRows * DP * 2, kPerRow = DP / 8, kLoads = kRows * kPerRow / kBlock, kApart = kBlock / kPerRow;
+  static constexpr size_t kLds = 2 * (size_t)(kStage + kRows * 4);
+};
 
-// More rows: the positions stay in registers, 32 NT for each of four wavefronts, and the rows come by in stages of 64 that all of
-// them share.
-template <class T, int DP, int NT, bool kExact>
-__global__ __launch_bounds__(kBlock, DP <= 128 ? 2 : 1) void weigh_many_kernel(WeighArgs a) {
-  constexpr int KS = DP / 16, kSpan = 32 * NT * (kBlock / 64), kStage = kStageRows * DP * 2;
-  __shared__ __attribute__((aligned(1024))) char stages[2 * kStage];
-  __shared__ __attribute__((aligned(16))) float lses[2][kStageRows];
-  lds_char *const lds = (lds_char *)stages;
+// Four wavefronts a SIMD where their registers allow it: 16 sessions, 8 heads of 8, 16 nodes after 3000 positions 35.0 us, with
+// three 38.7; 512 nodes after 8192 63 and 60 us.
+template <class T, int DP, bool kExact>
+__global__ __launch_bounds__(kBlock, DP <= 128 ? 4 : 2) void weigh_many_kernel(WeighArgs a) {
+  using Shape = ManyShape<DP>;
+  constexpr int KS = DP / 16, kRows = Shape::kRows, kSpan = Shape::kSpan, kStage = Shape::kStage, kLoads = Shape::kLoads,
+                kApart = Shape::kApart, kPerRow = Shape::kPerRow;
+  // two stages, then [2][kRows] of the rows' log-sum-exp.  (Through pointers to LDS: the compiler takes others for readers of what
+  // the loads in flight write, and would wait for those.)
+  extern __shared__ __attribute__((aligned(1024))) char weigh_lds[];
+  lds_char *const lds = (lds_char *)weigh_lds;
   const PoolView &p = a.p;
   const int pair = (int)(blockIdx.x % (uint32_t)a.pairs), s = pair / p.H, h = pair - s * p.H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
   const SessionView v = session_of(a, s, pair % p.H == 0 && blockIdx.x < (uint32_t)a.pairs);
   if (!v.ok) return;
-  const int32_t ctx = v.len - v.t, R = v.t * a.G;
+  const int32_t ctx = v.len - v.t;
   const int32_t *const table = p.table + (int64_t)s * p.M;
   const uint16_t *const keys = p.k + a.layer * p.layer_s + h * p.head_s + 8 * half;
   float *const weights = a.w.w + s * a.w.sess_s + a.layer * a.w.layer_s + h * a.w.head_s;
@@ -179,139 +194,182 @@ __global__ __launch_bounds__(kBlock, DP <= 128 ? 2 : 1) void weigh_many_kernel(W
   const uint16_t *const queries = a.q + v.n0 * a.q_node + (int64_t)h * a.G * a.q_head;
   const float *const lse = a.lse + (int64_t)v.n0 * (p.H * a.G) + h * a.G;
 
-  // this thread's pieces of a stage
-  constexpr int kPerRow = DP / 8, kLoads = kStageRows * kPerRow / kBlock, kApart = kStageRows / kLoads;  // rows between its loads
-  const int my_row = (int)threadIdx.x / kPerRow;
   if (!kExact) {  // pieces behind the last component are never loaded: zeros
-    for (int i = threadIdx.x * 16; i < 2 * kStage; i += kBlock * 16) *reinterpret_cast<uint4 *>(stages + i) = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x * 16; i < 2 * kStage; i += kBlock * 16) *reinterpret_cast<uint4 *>(weigh_lds + i) = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
   }
-  const auto request = [&](int32_t r0, int buf) {
+  // A stage is `nodes` whole nodes, or where a node has more heads than a stage has rows `heads` of one: its row r is node r / heads, head
+  // r % heads, at a distance from the stage's first that stays, so that the way from stage to stage is a scalar.  Rows behind
+  // those are filled with one of them, and weigh nothing: their log-sum-exp is infinite.
+  const int32_t parts = (a.G + kRows - 1) / kRows, heads = (a.G + parts - 1) / parts, nodes = max(1, kRows / a.G);
+  const int32_t stages = (v.t + nodes - 1) / nodes * parts;
+  struct Stage {
+    int32_t node0, head0;
+  };
+  const auto begin_of = [&](int32_t stage) {
+    if (parts == 1) return Stage{stage * nodes, 0};
+    return Stage{stage / parts, stage % parts * heads};
+  };
+  int32_t my_node[kLoads], my_head[kLoads];
+  int64_t my_at[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int row = (int)threadIdx.x / kPerRow + j * kApart, c = ((int)threadIdx.x % kPerRow) ^ turn<DP>(row), r = min(row, nodes * heads - 1);
+    my_node[j] = r / heads, my_head[j] = r - my_node[j] * heads;
+    my_at[j] = my_node[j] * a.q_node + my_head[j] * a.q_head + c * 8;
+  }
+  const int32_t lse_row = min((int)threadIdx.x, nodes * heads - 1), lse_node = lse_row / heads, lse_head = lse_row - lse_node * heads;
+  const int64_t lse_at = (int64_t)lse_node * (p.H * a.G) + lse_head;
+  int q_at[KS];  // of a stage: this lane's fragments (the turns of 32 rows repeat)
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) q_at[ks] = place<DP>(col, 2 * ks + half);
+  float next_lse = 0.0f;
+  const auto request = [&](Stage st, int buf) {
+    const bool full = st.node0 + nodes <= v.t && st.head0 + heads <= a.G;
+    const uint16_t *const base = queries + st.node0 * a.q_node + st.head0 * a.q_head;
+    // (every lane loads one, and first: a wait for it must not be one for the stage)
+    int64_t at_lse = lse_at;
+    if (!full) at_lse = (int64_t)min(lse_node, v.t - 1 - st.node0) * (p.H * a.G) + min(lse_head, a.G - 1 - st.head0);
+    next_lse = lse[(int64_t)st.node0 * (p.H * a.G) + st.head0 + at_lse];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int row = my_row + j * kApart, c = ((int)threadIdx.x % kPerRow) ^ turn<DP>(row);
-      const int32_t r = min(r0 + row, R - 1), node = r / a.G, g = r - node * a.G;
-      const uint16_t *const from = queries + node * a.q_node + g * a.q_head + c * 8;
-      lds_char *const to = lds + buf * kStage + (j * kBlock + wave * 64) * 16;
+      const int row = (int)threadIdx.x / kPerRow + j * kApart, c = ((int)threadIdx.x % kPerRow) ^ turn<DP>(row);
+      int64_t at = my_at[j];
+      if (!full) at = min(my_node[j], v.t - 1 - st.node0) * a.q_node + min(my_head[j], a.G - 1 - st.head0) * a.q_head + c * 8;
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass of the compiler does not know the device's load-to-LDS builtin
-      if (kExact || c < p.d8) __builtin_amdgcn_global_load_lds(from, to, 16, 0, 0);
+      if (kExact || c < p.d8) __builtin_amdgcn_global_load_lds(base + at, lds + buf * kStage + (j * kBlock + wave * 64) * 16, 16, 0, 0);
 #else
-      (void)from, (void)to;
+      (void)at, (void)c, (void)base, (void)lds, (void)buf;
 #endif
     }
-  };
-  const auto lse_of = [&](int32_t r0) {
-    const int32_t r = min(r0 + ((int)threadIdx.x & (kStageRows - 1)), R - 1), node = r / a.G;
-    return lse[(int64_t)node * (p.H * a.G) + r - node * a.G] * kLog2e;
   };
 
   const int32_t step = (int32_t)(gridDim.x / (uint32_t)a.pairs);
   for (int32_t chunk = (int32_t)(blockIdx.x / (uint32_t)a.pairs); (int64_t)chunk * kSpan < v.len; chunk += step) {
-    const int32_t first = chunk * kSpan + wave * 32 * NT;
-    // rows before those of the node at the workgroup's first position see none of them
-    const int32_t row0 = max(0, chunk * kSpan - ctx) * a.G / kStageRows * kStageRows;
-    request(row0, 0);
-    float next_lse = lse_of(row0);
-    short8v kf[NT][KS];
-    bool page_ok[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int32_t at = min(first + 32 * n + col, v.len - 1), page = table[at >> p.shift];
-      page_ok[n] = p.page_ok(page);
-      const uint16_t *const k = keys + (page_ok[n] ? page : 0) * p.page_s + (at & row_mask) * p.row_s;
+    const int32_t first = chunk * kSpan + wave * 32, pos = first + col;
+    // nodes before that at the workgroup's first position see none of them
+    int32_t stage = max(0, chunk * kSpan - ctx) / nodes * parts;
+    Stage here = begin_of(stage);
+    request(here, 0);
+    short8v kf[KS];
+    bool page_ok;
+    {
+      const int32_t at = min(pos, v.len - 1), page = table[at >> p.shift];
+      page_ok = p.page_ok(page);
+      const uint16_t *const k = keys + (page_ok ? page : 0) * p.page_s + (at & row_mask) * p.row_s;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        kf[n][ks] = short8v{};
-        if (kExact || 16 * ks + 8 * half < 8 * p.d8) kf[n][ks] = *reinterpret_cast<const short8v *>(k + 16 * ks);
+        kf[ks] = short8v{};
+        if (kExact || 16 * ks + 8 * half < 8 * p.d8) kf[ks] = *reinterpret_cast<const short8v *>(k + 16 * ks);
       }
     }
-    float sums[NT] = {};
-    int buf = 0;
-    for (int32_t r0 = row0; r0 < R; r0 += kStageRows, buf ^= 1) {
-      if (threadIdx.x < kStageRows) lses[buf][threadIdx.x] = next_lse;
+    // K has come before the loop begins: waited for inside it, it would take the loads under way along
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(kf[ks]));
+    float sum = 0.0f;
+    for (int buf = 0; stage < stages; ++stage, buf ^= 1) {
+      // rows of this stage that are some, and those in front that do not see all of the wavefront's positions
+      const int32_t node0 = here.node0, some = min(nodes, v.t - node0) * min(heads, a.G - here.head0);
+      const int32_t blind = max(0, first + 31 - ctx - node0) * heads;
+      lds_char *const stage_lse = lds + 2 * kStage + buf * kRows * 4;
+      if (threadIdx.x < kRows) *(lds_float *)(stage_lse + 4 * threadIdx.x) = (int)threadIdx.x < some ? next_lse * kLog2e : __builtin_inff();
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the compiler does not wait for loads to LDS at a barrier)
       __syncthreads();  // this stage has come, and everybody is done with the one before
-      if (r0 + kStageRows < R) {
-        request(r0 + kStageRows, buf ^ 1);
-        next_lse = lse_of(r0 + kStageRows);
-      }
+      here = begin_of(stage + 1);
+      if (stage + 1 < stages) request(here, buf ^ 1);
 #pragma unroll
-      for (int m = 0; m < kStageRows / 32; ++m) {
-        float16v sc[NT];
+      for (int m = 0; m < kRows / 32; ++m) {
+        if (32 * m >= some) break;
+        float16v sc;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+        // Q's fragments four products ahead; fences keep the order
+        short8v qf[2][4];
+        const auto read_q = [&](int g) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sc[n][i] = 0.0f;
+          for (int ks = 4 * g; ks < 4 * g + 4; ++ks)
+            qf[g & 1][ks & 3] = *(const __attribute__((address_space(3))) short8v *)(lds + buf * kStage + 32 * m * (DP * 2) + q_at[ks]);
+        };
+        read_q(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const short8v qf = *(const __attribute__((address_space(3))) short8v *)(lds + buf * kStage + place<DP>(32 * m + col, 2 * ks + half));
+        for (int g = 0; g < KS / 4; ++g) {
+          if (g + 1 < KS / 4) read_q(g + 1);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) sc[n] = mfma<T>(qf, kf[n][ks], sc[n]);
+          for (int ks = 4 * g; ks < 4 * g + 4; ++ks) sc = mfma<T>(qf[g & 1][ks & 3], kf[ks], sc);
+          __builtin_amdgcn_sched_barrier(0);
         }
         float lse2[16];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const float4 x = *reinterpret_cast<const float4 *>(&lses[buf][32 * m + 8 * g + 4 * half]);
-          lse2[4 * g] = x.x, lse2[4 * g + 1] = x.y, lse2[4 * g + 2] = x.z, lse2[4 * g + 3] = x.w;
+          const float4v x = *(const __attribute__((address_space(3))) float4v *)(stage_lse + 4 * (32 * m + 8 * g + 4 * half));
+#pragma unroll
+          for (int b = 0; b < 4; ++b) lse2[4 * g + b] = x[b];
         }
-        const int32_t r1 = r0 + 32 * m;
-        // all of these rows are some, and see all of the wavefront's positions
-        const bool whole = r1 + 32 <= R && (int64_t)(first + 32 * NT - 1 - ctx) * a.G <= r1;
+        float part[2] = {0.0f, 0.0f};  // a tile's rows by themselves first: a long sum loses less
+        if (blind <= 32 * m) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float part[2] = {0.0f, 0.0f};  // a tile's rows by themselves first: a long sum loses less
-          if (whole) {
+          for (int i = 0; i < 16; ++i) part[i & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale2, -lse2[i]));
+        } else {
+          // a bit for each row that is one and sees this lane's position: from `lo` on, below `hi`
+          const int lo = min(max(max(0, pos - ctx - node0) * heads - 32 * m, 0), 32), hi = min(some - 32 * m, 32);
+          const uint32_t sees = (uint32_t)(((1ull << hi) - 1) & ~((1ull << lo) - 1)) >> (4 * half);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) part[i & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], a.scale2, -lse2[i]));
-          } else {
-            const int64_t my_first = (int64_t)max(0, first + 32 * n + col - ctx) * a.G;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int32_t r = r1 + 8 * (i >> 2) + 4 * half + (i & 3);
-              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], a.scale2, -lse2[i]));
-              part[i & 1] += r < R && r >= my_first ? w : 0.0f;
-            }
+          for (int i = 0; i < 16; ++i) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale2, -lse2[i]));
+            part[i & 1] += sees >> (8 * (i >> 2) + (i & 3)) & 1u ? w : 0.0f;
           }
-          sums[n] += part[0] + part[1];
         }
+        sum += part[0] + part[1];
       }
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float sum = sums[n] + __shfl_xor(sums[n], 32);
-      const int32_t pos = first + 32 * n + col;
-      if (pos < v.len && half == 0) {
-        if (page_ok[n]) put_weight(a, weights + pos, pos < ctx, a.decay != 0.0f ? weights[pos] : 0.0f, sum);
-        else raise(a.status, PLC_ERR_INVALID);
-      }
+    sum += __shfl_xor(sum, 32);
+    if (pos < v.len && half == 0) {
+      if (page_ok) put_weight(a, weights + pos, pos < ctx, a.decay != 0.0f ? weights[pos] : 0.0f, sum);
+      else raise(a.status, PLC_ERR_INVALID);
     }
     __syncthreads();  // the next chunk's first stage goes where others may still read
   }
 }
 
-template <class K>
-void launch_weigh(const K &kernel, WeighArgs a, int64_t span, hipStream_t st) {
+int64_t groups_of(const WeighArgs &a, int64_t span) {
   const int64_t chunks = (a.max_len + span - 1) / span, most = (kMostGroups + a.pairs - 1) / a.pairs;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.pairs * (chunks < most ? chunks : most))), dim3(kBlock), 0, st, a);
+  return a.pairs * (chunks < most ? chunks : most);
 }
 
+template <class T, int DP, int kTiles>
+void launch_few(const WeighArgs &a, hipStream_t st) {
+  hipLaunchKernelGGL((weigh_few_kernel<T, DP, kTiles>), dim3((unsigned)groups_of(a, kTiles * kSpanOfGroup)), dim3(kBlock), 0, st, a);
+}
+
+template <class T, int DP, bool kExact>
+void launch_many(const WeighArgs &a, hipStream_t st) {
+  constexpr size_t lds = ManyShape<DP>::kLds;
+  if (lds > 64 * 1024) {
+    static std::atomic<uint64_t> sized{0};  // devices that know of the kernel's LDS: to tell them costs a call's host time over again
+    int device = 0;
+    (void)hipGetDevice(&device);
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (!(sized.load(std::memory_order_relaxed) & bit)) {
+      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&weigh_many_kernel<T, DP, kExact>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      sized.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  hipLaunchKernelGGL((weigh_many_kernel<T, DP, kExact>), dim3((unsigned)groups_of(a, kSpanOfGroup)), dim3(kBlock), lds, st, a);
+}
+
+// Four tiles a wavefront where there are that many: 64 sessions, 8 heads of 4, one token after up to 4096 positions 78 us, with one tile 93, two 85,
+// eight 79; 20 sessions of 24,323 positions 214, 244, 232 and 212.
 template <class T, int DP>
 void weigh(const WeighArgs &a, hipStream_t st) {
   const int64_t tiles = (int64_t)a.pairs * ((a.max_len + 31) / 32);
-  constexpr int kMany = DP <= 128 ? 4 : 2;
-  if ((int64_t)a.max_nodes * a.G <= 32) {
-    if (tiles >= 16 * 1024) launch_weigh(&weigh_few_kernel<T, DP, kMany>, a, 32 * 4 * kMany, st);
-    else launch_weigh(&weigh_few_kernel<T, DP, 1>, a, 32 * 4, st);
-    return;
-  }
-  const bool exact = 8 * a.p.d8 == DP;
-  constexpr int NT = DP <= 128 ? 2 : 1;
-  if (DP <= 128 && tiles >= 8 * 1024) {
-    if (exact) launch_weigh(&weigh_many_kernel<T, DP, NT, true>, a, 128 * NT, st);
-    else launch_weigh(&weigh_many_kernel<T, DP, NT, false>, a, 128 * NT, st);
+  if ((int64_t)a.max_nodes * a.G > 32) {
+    if (8 * a.p.d8 == DP) launch_many<T, DP, true>(a, st);
+    else launch_many<T, DP, false>(a, st);
+  } else if (tiles >= 64 * kComputeUnits) {
+    launch_few<T, DP, DP <= 128 ? 4 : 2>(a, st);
   } else {
-    if (exact) launch_weigh(&weigh_many_kernel<T, DP, 1, true>, a, 128, st);
-    else launch_weigh(&weigh_many_kernel<T, DP, 1, false>, a, 128, st);
+    launch_few<T, DP, 1>(a, st);
   }
 }
 
