@@ -763,7 +763,7 @@ int plc_rotary_turns(const double *theta /* host */, int32_t pairs, uint64_t *tu
 
 /* Rows of a buffer: x, out logical [rows, heads, d] (element strides of row and head, multiples of 8; 16-byte aligned), out may
  * be x, with the same strides; else they must not overlap.  positions i32 [rows].  inverse: turned by -a and divided by the
- * magnitude.  d a multiple of 8, up to 2048; rows < 2^31, heads * d < 2^31. */
+ * magnitude.  d a multiple of 8, up to 2048; rows * d < 2^35, heads * d < 2^31. */
 int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x, const int64_t *x_stride /* host */,
                int64_t rows, int32_t heads, int32_t d, const int32_t *positions, int32_t inverse, void *out,
                const int64_t *out_stride /* host */, void *stream);
@@ -775,8 +775,8 @@ int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x,
  *   rel    nullable: i32, one for each row of the buffer (rows, or S * rows); i without.  A drafted tree's nodes: their depths.
  *   q, q_out   nullable, with packed rows: logical [rows->rows, H*G, d], strides (node, head) and alignment as for
  *          plc_attend; q_out may be q, with the same strides.
- * Rows that cannot be stored (status) are left alone, in q_out too, and so are rows behind off[S].  d up to 2048;
- * layers * H and H * G < 2^29. */
+ * Rows that cannot be stored (status) are left alone, in q_out too, and so are rows behind off[S].  d up to 2048,
+ * rows (of all sessions) * d < 2^35, layers * H and H * G < 2^29. */
 int plc_rotate_store(const plc_pages *pages /* host */, const plc_rows *rows /* host */, const plc_rotary *rotary /* host */,
                      int32_t type, const int32_t *off, const int32_t *base, const int32_t *rel, const void *k, const void *v,
                      const void *q, const int64_t *q_stride /* host */, int32_t G, void *q_out,
@@ -844,7 +844,7 @@ int plc_pages_evict(const plc_pages *pages /* host */, const int32_t *keep, int3
  * status PLC_ERR_INVALID; its results are NaN, and ids and chosen -1.  A token that is none raises it too: logprob NaN,
  * chosen -1.  All sums in fp32.
  *   type     PLC_FP16, PLC_BF16 or PLC_FP32, of the logits.  Rows at `row_stride` elements, aligned as their elements are.
- *   V        1..2^30.  N >= 0, N < 2^31.  k 0..32, at most V.
+ *   V        1..2^30.  N >= 0, N < 2^24.  k 0..32, at most V.
  *   tokens   nullable: i32 [N].
  *   logprob, entropy, lse   out, nullable: fp32 [N].  logprob, chosen: only with tokens.
  *   ids, top_logprobs, probs, chosen   out, nullable: [N, k], chosen i32 [N].

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <cstdio>
 
 #include "plc.h"
@@ -178,6 +179,19 @@ int patch_escapes(const plc_dims *dims, const uint8_t *symbols, const uint16_t *
                   hipStream_t st, bool launch = true);
 
 inline int launch_status() { return hipGetLastError() == hipSuccess ? PLC_OK : PLC_ERR_HIP; }
+
+// Lets a kernel have more than 64 KB of LDS (`bytes`, always the same) on the current device.  `told`: the devices that know, as to tell
+// them costs a call's host time over again.
+template <class Kernel>
+inline void allow_lds(Kernel kernel, size_t bytes, std::atomic<uint64_t> *told) {
+  if (bytes <= 64 * 1024) return;
+  int device = 0;
+  (void)hipGetDevice(&device);
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (told->load(std::memory_order_relaxed) & bit) return;
+  (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  told->fetch_or(bit, std::memory_order_relaxed);
+}
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

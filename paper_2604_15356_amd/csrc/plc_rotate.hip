@@ -246,7 +246,7 @@ int launch_rotate(RotateArgs a, int64_t rows, int64_t heads, hipStream_t st) {
   while (a.block_rows > 1 && a.block_rows / 2 >= rows) a.block_rows /= 2;
   a.slots = units / a.block_rows;
   const int64_t bx = (rows + a.block_rows - 1) / a.block_rows;
-  if (bx > INT32_MAX) return PLC_ERR_INVALID;
+  if (bx >= 1 << 24) return PLC_ERR_INVALID;  // (lanes of a launch < 2^32)
   const int64_t most = (heads + a.slots - 1) / a.slots;
   int64_t by = (8 * kComputeUnits + bx - 1) / bx;
   by = by > most ? most : by;

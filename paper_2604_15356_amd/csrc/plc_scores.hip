@@ -5,15 +5,17 @@
 // T = sum a 2^a, a = c x - c m with c = scale * log2(e): then lse = ln 2 (c m + log2 Z) and the entropy is ln 2 (log2 Z - T / Z).
 // c m is rounded once, and the same number is taken from every c x by a fused product, so that its rounding drops out.
 //
-// The k largest come out of the maxima that are there anyway.  Call the 256 sets of pieces that the threads (or fours of them)
-// have seen groups.  The group with the k-th largest maximum bounds what can be among the k largest from below: at least k
-// logits are as large.  So only groups whose maximum is that large hold any, and there are exactly k of them where maxima that are equal
-// are told apart by the piece they stand in first.  Those k groups are read again, k in 256 of the row, from the caches, and
-// what lies above the bound goes into a list in LDS that is ranked by counting.  Keys are 64 bits, the logit as an ordered whole
-// number over the token's complement: no two are equal, so that the result does not depend on the order they came in.
+// The k largest: call what each of 64 fours of threads has seen a group.  The group with the k-th largest maximum bounds the k
+// largest from below: at least k logits are as large.  What is not below it goes into a list in LDS: a thread looks its pieces through
+// where they are all in its registers still; else it reads the piece that holds its maximum again, or all that it has seen, where
+// the largest of its other pieces, which it has kept too, is not below the bound.  The list is ranked by counting.  Where it
+// has no room for all (many large logits with few threads), the row is gone through again and the list shortened on the way.
+// Keys are 64 bits, the logit as an ordered whole number over the token's complement: no two are equal, so that the
+// result does not depend on the order they came in.
 //
-// What bounds it: HBM for many rows, for which one workgroup a row suffices; latency for few, whose rows are cut into parts
-// that a second kernel joins.
+// What bounds it: HBM for many rows (4096 rows of 50,016 bf16 logits, 410 MB, k = 8: 83 us, 4.9 TB/s; k = 0: 77 us, k = 32: 87), a
+// workgroup for each; for few the host's time, and behind that the stages of one workgroup (a row of 50,016, k = 4: 9.4 us, of which the
+// load 2, sums and maxima 3, the k largest 3).  Long rows, where they are few, are cut into parts that a second kernel joins.
 #include <type_traits>
 
 #include "plc_device.h"
@@ -24,8 +26,9 @@ namespace {
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 constexpr float kNothing = -1e30f;  // c m before anything was seen; beyond +-it c x may overflow, and the row is gone through again
 constexpr float kGone = -200.0f;    // 2^kGone is zero
-constexpr int kGroups = 256, kMostK = 32, kMostParts = 32;
+constexpr int kGroups = 64, kMostK = 32, kMostParts = 32;
 constexpr int64_t kPartRows = 512;  // workgroups that rows are cut into parts for
+constexpr int64_t kLongRow = 8192;  // pieces of a row that is
 
 struct ScoreArgs {
   const char *logits;
@@ -82,6 +85,7 @@ struct Logits {
     for (int e = 0; e < E; ++e) v[e] = j + e >= 0 && j + e < V ? row[j + e] : (T)-__builtin_inff();
     return __builtin_bit_cast(uint4, v);
   }
+  __device__ __forceinline__ uint4 whole(int32_t piece) const { return *reinterpret_cast<const uint4 *>(row + first_of(piece)); }
   static __device__ __forceinline__ void unpack(uint4 raw, float (&x)[E]) {
     typedef T T8 __attribute__((ext_vector_type(E)));
     const T8 v = __builtin_bit_cast(T8, raw);
@@ -90,15 +94,26 @@ struct Logits {
   }
 };
 
+// Maximum and sum over the 64 lanes of a wavefront, the same in every lane: through the lanes' own registers, as wave_inclusive_scan.
+template <int kControl, int kRows>
+__device__ __forceinline__ float from_lane(float v, float otherwise) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, otherwise), __builtin_bit_cast(int, v), kControl, kRows, 0xf, false));
+}
+template <class Join>
+__device__ __forceinline__ float wave_join(float v, float nothing, Join join) {
+  v = join(v, from_lane<0x111, 0xf>(v, nothing));  // row_shr:1
+  v = join(v, from_lane<0x112, 0xf>(v, nothing));  // row_shr:2
+  v = join(v, from_lane<0x114, 0xf>(v, nothing));  // row_shr:4
+  v = join(v, from_lane<0x118, 0xf>(v, nothing));  // row_shr:8
+  v = join(v, from_lane<0x142, 0xa>(v, nothing));  // row_bcast:15 into rows 1 and 3
+  v = join(v, from_lane<0x143, 0xc>(v, nothing));  // row_bcast:31 into rows 2 and 3
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return wave_join(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_add(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  return wave_join(v, 0.0f, [](float a, float b) { return a + b; });
 }
 
 // Brings sums from one reference to another, `d` below it.
@@ -116,19 +131,23 @@ struct List {
   uint32_t count;
 };
 
-// Ranks the list: its k largest to its front, and in order in `top` (zero where there are fewer).
-template <int kThreads, int kCap>
+// Ranks the list: its k largest in order in `top` (zero where there are fewer), and unless it is the last time to its front.
+template <bool kLast, int kCap>
 __device__ __forceinline__ void rank(List<kCap> &list, int32_t k) {
   const uint32_t n = list.count;
-  if (threadIdx.x < kMostK) list.top[threadIdx.x] = 0;
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+  if (n < (uint32_t)k) {
+    if (threadIdx.x < kMostK) list.top[threadIdx.x] = 0;
+    __syncthreads();
+  }
+  for (uint32_t i = threadIdx.x; i < n; i += kBlock) {
     const uint64_t mine = list.keys[i];
     uint32_t above = 0;
+#pragma unroll 8
     for (uint32_t j = 0; j < n; ++j) above += list.keys[j] > mine;
     if (above < (uint32_t)k) list.top[above] = mine;
   }
   __syncthreads();
+  if (kLast) return;
   if (threadIdx.x < (uint32_t)k) list.keys[threadIdx.x] = list.top[threadIdx.x];
   if (threadIdx.x == 0) {
     list.count = min(n, (uint32_t)k);
@@ -172,21 +191,21 @@ __device__ __forceinline__ void finish(const ScoreArgs &a, int64_t x, const Stat
   }
 }
 
-template <class T, int kThreads>
+template <class T>
 struct ScoreShape {
-  static constexpr int E = Logits<T>::E, kLimit = 256, kCap = kThreads * E + kLimit;
+  static constexpr int E = Logits<T>::E, kLimit = 256, kCap = kBlock * E + kLimit;  // of the list: shortened at; room
+  static constexpr int kUnroll = 4, kRound = kBlock * kUnroll;  // pieces under way of a thread, of a workgroup
 };
 
 // A row, or a part of one, to a workgroup.
-template <class T, int kThreads>
-__global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
-  using Shape = ScoreShape<T, kThreads>;
-  constexpr int E = Shape::E, kUnroll = 4, kWaves = kThreads / 64, kOf = kThreads / kGroups;
-  extern __shared__ __attribute__((aligned(16))) char score_lds[];
-  auto &list = *reinterpret_cast<List<Shape::kCap> *>(score_lds);
+template <class T>
+__global__ __launch_bounds__(kBlock) void score_kernel(ScoreArgs a) {
+  using Shape = ScoreShape<T>;
+  constexpr int E = Shape::E, kUnroll = Shape::kUnroll, kRound = Shape::kRound, kWaves = kBlock / 64, kOf = kBlock / kGroups;
+  __shared__ List<Shape::kCap> list;
   __shared__ float meet[3][kWaves];
-  __shared__ uint64_t group_key[kGroups];
-  __shared__ int32_t group[kMostK];
+  __shared__ __attribute__((aligned(16))) uint64_t group_key[kGroups];
+  __shared__ int32_t holders[kMostK * kOf], n_holders;
   __shared__ int32_t found;
   const int64_t x = blockIdx.x / (uint32_t)a.parts;
   const int32_t part = (int32_t)(blockIdx.x - (uint32_t)x * (uint32_t)a.parts);
@@ -194,16 +213,39 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
   const int32_t each = (row.pieces + a.parts - 1) / a.parts;
   const int32_t q0 = min(row.pieces, part * each), q1 = min(row.pieces, q0 + each);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  constexpr uint32_t kInf = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, _Float16>::value ? 0xfc00fc00u : 0xff80ff80u;  // minus infinity
+  if (threadIdx.x == 0) list.count = 0, list.bound = 0, n_holders = 0;
 
-  float best = -__builtin_inff(), shift = kNothing, z = 0.0f, t = 0.0f;
-  int32_t best_piece = -1;
-  for (int32_t j0 = q0 + (int32_t)threadIdx.x; j0 < q1; j0 += kThreads * kUnroll) {
-    uint4 raw[kUnroll];
-    constexpr uint32_t kInf = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, _Float16>::value ? 0xfc00fc00u : 0xff80ff80u;
+  // A piece's logits that may be among the k largest, to the list; not those that it has no room for, which its length tells.
+  const auto take = [&](uint4 piece, int32_t j, uint64_t bound, float least) {
+    float v[E];
+    Logits<T>::unpack(piece, v);
+    const int32_t first = row.first_of(j);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      raw[u] = j0 + u * kThreads < q1 ? row.load(j0 + u * kThreads) : make_uint4(kInf, kInf, kInf, kInf);
-    float top = best;
+    for (int e = 0; e < E; ++e) {
+      if (!(v[e] >= least)) continue;
+      const uint64_t key = key_of(v[e], 0xffffffffu - (uint32_t)(first + e));
+      if (key < bound || first + e < 0 || first + e >= a.V) continue;
+      const uint32_t at = atomicAdd(&list.count, 1u);
+      if (at < (uint32_t)Shape::kCap) list.keys[at] = key;
+    }
+  };
+
+  // this thread's largest logit, the first piece that holds it, and the largest of the other pieces
+  float best = -__builtin_inff(), second = -__builtin_inff(), shift = kNothing, z = 0.0f, t = 0.0f;
+  int32_t best_piece = q0 + (int32_t)threadIdx.x < q1 ? q0 + (int32_t)threadIdx.x : -1;
+  uint4 raw[kUnroll];
+  const bool ragged = row.mis != 0 || row.first_of(row.pieces) != row.V;  // its first or its last piece is not all its own
+  for (int32_t r0 = q0; r0 < q1; r0 += kRound) {
+    const int32_t j0 = r0 + (int32_t)threadIdx.x;
+    if (r0 + kRound <= q1 && !(ragged && (r0 == 0 || r0 + kRound >= row.pieces))) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) raw[u] = row.whole(j0 + u * kBlock);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) raw[u] = j0 + u * kBlock < q1 ? row.load(j0 + u * kBlock) : make_uint4(kInf, kInf, kInf, kInf);
+    }
+    const float before = best;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       float v[E];
@@ -211,11 +253,12 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
       float most = v[0];
 #pragma unroll
       for (int e = 1; e < E; ++e) most = fmaxf(most, v[e]);
-      if (most > top || best_piece < 0) top = fmaxf(most, top), best_piece = j0 + u * kThreads;
+      best_piece = most > best ? j0 + u * kBlock : best_piece;
+      second = fmaxf(second, fminf(most, best));
+      best = fmaxf(most, best);
     }
-    if (top > best) {
-      best = top;
-      const float now = top * a.scale2;
+    if (best > before) {
+      const float now = best * a.scale2;
       if (now > shift) {
         rebase(shift - now, &z, &t);
         shift = now;
@@ -237,7 +280,15 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
 
   // the workgroup's
   Stats s = {};
+  const uint64_t mine = best_piece < 0 ? 0 : key_of(best, 0xffffffffu - (uint32_t)(row.first_of(best_piece) + E - 1));
   {
+    uint64_t key = mine;
+#pragma unroll
+    for (int d = 1; d < kOf; d <<= 1) {
+      const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)key, d);
+      key = other > key ? other : key;
+    }
+    if (threadIdx.x % kOf == 0) group_key[threadIdx.x / kOf] = key;
     const float m = wave_max(best);
     if (lane == 0) meet[0][wave] = m;
     __syncthreads();
@@ -249,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
     if (finite && !(fabsf(s.shift) < -kNothing)) {  // out of range: once more, from the largest
       s.base = s.best, s.shift = 0.0f;
       z = t = 0.0f;
-      for (int32_t j = q0 + (int32_t)threadIdx.x; j < q1; j += kThreads) {
+      for (int32_t j = q0 + (int32_t)threadIdx.x; j < q1; j += kBlock) {
         float v[E];
         Logits<T>::unpack(row.load(j), v);
 #pragma unroll
@@ -264,57 +315,70 @@ __global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a) {
     }
     z = wave_add(z), t = wave_add(t);
     if (lane == 0) meet[1][wave] = z, meet[2][wave] = t;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) s.z += meet[1][w], s.t += meet[2][w];
   }
-
   if (a.k > 0) {
-    uint64_t mine = best_piece < 0 ? 0 : key_of(best, 0xffffffffu - (uint32_t)(row.first_of(best_piece) + E - 1));
-#pragma unroll
-    for (int d = 1; d < kOf; d <<= 1) {
-      const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)mine, d);
-      mine = other > mine ? other : mine;
-    }
-    if (threadIdx.x % kOf == 0) group_key[threadIdx.x / kOf] = mine;
-    if (threadIdx.x == 0) list.count = 0, list.bound = 0;
-    if (threadIdx.x < kMostK) group[threadIdx.x] = -1;
-    __syncthreads();
-    if (threadIdx.x < kGroups) {
-      mine = group_key[threadIdx.x];
+    {  // the group with the k-th largest maximum: kOf threads compare one with all
+      const uint64_t key = group_key[threadIdx.x / kOf];
+      const int g0 = (int)threadIdx.x % kOf * (kGroups / kOf);
       int32_t above = 0;
-#pragma unroll 8
-      for (int g = 0; g < kGroups; ++g) {
-        const uint64_t other = group_key[g];
-        above += other > mine || (other == mine && g < (int)threadIdx.x);  // (equal: only those without a piece)
-      }
-      if (above < a.k && mine != 0) {
-        group[above] = (int32_t)threadIdx.x;
-        if (above == a.k - 1) list.bound = mine;
-      }
+#pragma unroll
+      for (int i = 0; i < kGroups / kOf; ++i) above += group_key[g0 + i] > key;
+#pragma unroll
+      for (int d = 1; d < kOf; d <<= 1) above += __shfl_xor(above, d);
+      if (threadIdx.x % kOf == 0 && above == a.k - 1 && key != 0) list.bound = key;  // (no two are equal, but of groups without a piece)
     }
     __syncthreads();
-    const int32_t rounds = (q1 - q0 + kThreads - 1) / kThreads, items = a.k * kOf * rounds;
-    for (int32_t i0 = 0; i0 < items; i0 += kThreads) {
-      const int32_t i = i0 + (int32_t)threadIdx.x, g = i / (kOf * rounds), rest = i - g * (kOf * rounds);
-      const int32_t of = i < items ? group[g] : -1;
-      const int32_t j = q0 + of * kOf + rest % kOf + rest / kOf * kThreads;
-      if (of >= 0 && j < q1) {
-        const uint64_t bound = list.bound;
-        float v[E];
-        Logits<T>::unpack(row.load(j), v);
-        const int32_t first = row.first_of(j);
+    const uint64_t bound = list.bound;
+    const float least = bound ? logit_of(bound) : -__builtin_inff();
+    const bool holds = mine >= bound && mine != 0;
+    const int32_t rounds = (q1 - q0 + kBlock - 1) / kBlock;
+    if (q1 - q0 <= kRound) {  // a thread's pieces are all in its registers
+      if (holds) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const uint64_t key = key_of(v[e], 0xffffffffu - (uint32_t)(first + e));
-          if (key >= bound && first + e >= 0 && first + e < a.V) list.keys[atomicAdd(&list.count, 1u)] = key;
+        for (int u = 0; u < kUnroll; ++u) {
+          const int32_t j = q0 + (int32_t)threadIdx.x + u * kBlock;
+          if (j < q1) take(raw[u], j, bound, least);
         }
       }
+    } else {
+      if (holds) {
+        if (second < least) take(row.load(best_piece), best_piece, bound, least);
+        else holders[atomicAdd(&n_holders, 1)] = (int32_t)threadIdx.x;  // (in any order: so is the list)
+      }
       __syncthreads();
-      if (i0 + kThreads < items && list.count > Shape::kLimit) rank<kThreads>(list, a.k);
+      for (int32_t i = (int32_t)threadIdx.x; i < n_holders * rounds; i += kBlock * kUnroll) {
+        int32_t j[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          const int32_t item = i + u * kBlock, h = item / rounds;
+          j[u] = item < n_holders * rounds ? q0 + holders[h] + (item - h * rounds) * kBlock : q1;
+          if (j[u] < q1) raw[u] = row.load(j[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (j[u] < q1) take(raw[u], j[u], bound, least);
+      }
     }
-    rank<kThreads>(list, a.k);
   }
+  __syncthreads();
+  const bool too_many = a.k > 0 && list.count > (uint32_t)Shape::kCap;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) s.z += meet[1][w], s.t += meet[2][w];
+  if (too_many) {  // all pieces again, and the list shortened, and with it the bound raised, where it grows long
+    if (threadIdx.x == 0) list.count = 0;
+    __syncthreads();
+    for (int32_t r0 = q0; r0 < q1; r0 += kBlock) {
+      const int32_t j = r0 + (int32_t)threadIdx.x;
+      const uint64_t bound = list.bound;
+      if (j < q1) take(row.load(j), j, bound, logit_of(bound));
+      __syncthreads();  // (nobody adds to the list before everybody has read how long it is)
+      const bool full = list.count > Shape::kLimit;
+      __syncthreads();
+      if (full) rank<false>(list, a.k);
+    }
+  }
+  if (a.k > 0) rank<true>(list, a.k);
   if (a.parts == 1) {
     finish<T>(a, x, s, list.top, &found);
     return;
@@ -351,31 +415,26 @@ __global__ __launch_bounds__(kBlock) void score_join_kernel(ScoreArgs a) {
   for (int32_t i = threadIdx.x; i < a.parts * a.k; i += kBlock)
     list.keys[i] = reinterpret_cast<const uint64_t *>(from + i / a.k * bytes + sizeof(Part))[i % a.k];
   __syncthreads();
-  if (a.k > 0) rank<kBlock>(list, a.k);
+  if (a.k > 0) rank<true>(list, a.k);
   const Stats s = joined;
   finish<T>(a, x, s, list.top, &found);
 }
 
-template <class T, int kThreads>
-void launch_scores(const ScoreArgs &a, hipStream_t st) {
-  constexpr size_t lds = sizeof(List<ScoreShape<T, kThreads>::kCap>);
-  if (lds > 32 * 1024)
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&score_kernel<T, kThreads>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  hipLaunchKernelGGL((score_kernel<T, kThreads>), dim3((unsigned)(a.N * a.parts)), dim3(kThreads), lds, st, a);
-}
-
 template <class T>
 int scores(ScoreArgs a, hipStream_t st) {
+  // A workgroup has a row of 50,016 16-bit logits in 9.4 us; in parts and with the joining 8.9, but a launch costs the host 3.3 more.  Of 131,072
+  // 15.6 against 10.2, of 300,000 30 against 12.7.  With more rows than half the compute units the chip is full as it is (300 rows of
+  // 50,016 in 32 bits: 16.7 against 19.1).
   const int64_t pieces = ((int64_t)a.V * sizeof(T) + 15) / 16;
   int64_t parts = 1;
-  if (a.N < kPartRows) {
+  if (2 * a.N <= kComputeUnits && pieces > kLongRow) {
     parts = (kPartRows + a.N - 1) / a.N;
-    const int64_t most = (pieces + 4 * kBlock - 1) / (4 * kBlock);
+    const int64_t most = (pieces + ScoreShape<T>::kRound - 1) / ScoreShape<T>::kRound;
     parts = parts > most ? most : parts;
     parts = parts > kMostParts ? kMostParts : parts;
   }
   a.parts = (int32_t)parts;
-  launch_scores<T, kBlock>(a, st);
+  hipLaunchKernelGGL(score_kernel<T>, dim3((unsigned)(a.N * a.parts)), dim3(kBlock), 0, st, a);
   if (a.parts > 1) hipLaunchKernelGGL(score_join_kernel<T>, dim3((unsigned)a.N), dim3(kBlock), 0, st, a);
   return launch_status();
 }
@@ -395,7 +454,7 @@ extern "C" int plc_score_tokens(int32_t type, const void *logits, int64_t row_st
                                 float *top_logprobs, float *probs, int32_t *chosen, void *ws, size_t ws_bytes, uint32_t *status,
                                 void *stream) {
   const auto fine = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; };  // (or null)
-  if ((type != PLC_FP16 && type != PLC_BF16 && type != PLC_FP32) || row_stride < 0 || N < 0 || N > INT32_MAX || !shape_ok(V, k) ||
+  if ((type != PLC_FP16 && type != PLC_BF16 && type != PLC_FP32) || row_stride < 0 || N < 0 || N >= 1 << 24 || !shape_ok(V, k) ||
       !(scale > 0.0f) || !(scale * kLog2e < __builtin_inff()) || !fine(tokens) || !fine(logprob) || !fine(entropy) || !fine(lse) ||
       !fine(ids) || !fine(top_logprobs) || !fine(probs) || !fine(chosen) || ((logprob || chosen) && !tokens) ||
       ((ids || top_logprobs || probs || chosen) && k == 0) || !status || reinterpret_cast<uintptr_t>(ws) % 256 || !ws ||

@@ -345,16 +345,8 @@ void launch_few(const WeighArgs &a, hipStream_t st) {
 template <class T, int DP, bool kExact>
 void launch_many(const WeighArgs &a, hipStream_t st) {
   constexpr size_t lds = ManyShape<DP>::kLds;
-  if (lds > 64 * 1024) {
-    static std::atomic<uint64_t> sized{0};  // devices that know of the kernel's LDS: to tell them costs a call's host time over again
-    int device = 0;
-    (void)hipGetDevice(&device);
-    const uint64_t bit = device < 64 ? 1ull << device : 0;
-    if (!(sized.load(std::memory_order_relaxed) & bit)) {
-      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&weigh_many_kernel<T, DP, kExact>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      sized.fetch_or(bit, std::memory_order_relaxed);
-    }
-  }
+  static std::atomic<uint64_t> told{0};
+  allow_lds(&weigh_many_kernel<T, DP, kExact>, lds, &told);
   hipLaunchKernelGGL((weigh_many_kernel<T, DP, kExact>), dim3((unsigned)groups_of(a, kSpanOfGroup)), dim3(kBlock), lds, st, a);
 }
 

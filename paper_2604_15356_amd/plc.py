@@ -829,20 +829,30 @@ _LOGIT_TYPES = {torch.float16: PLC_FP16, torch.bfloat16: PLC_BF16, torch.float32
 def plc_score_tokens(logits, scale, tokens, k, logprob, entropy, lse, ids, top_logprobs, probs, chosen, ws, status):
     """logits [N, V], the tokens contiguous; tokens int32 [N] or None; out, or None: logprob, entropy, lse float32 [N], ids int32 and
     top_logprobs, probs float32 [N, k], chosen int32 [N]."""
+    _on(_current_device(), logits, tokens, logprob, entropy, lse, ids, top_logprobs, probs, chosen, ws, status)
+    N = logits.shape[0]
+    for t, n in ((logprob, N), (entropy, N), (lse, N), (chosen, N), (ids, N * k), (top_logprobs, N * k), (probs, N * k)):
+        if t is not None and t.numel() != n:
+            raise ValueError("a result does not have a place for each row (and alternative)")
+    _score_tokens(logits, scale, tokens, k, *(_floats(t) for t in (logprob, entropy, lse)), _ints_or_none(ids), _floats(top_logprobs),
+                  _floats(probs), _ints_or_none(chosen), _on_device(ws), ws.numel(), _ints(status))
+
+
+def _score_tokens(logits, scale, tokens, k, *results):
+    """The same with the results' addresses, the workspace's, its size and the status'."""
     stream = _stream_of(logits)
-    _on(logits.get_device(), tokens, logprob, entropy, lse, ids, top_logprobs, probs, chosen, ws, status)
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits are [rows, tokens], the tokens contiguous")
-    if logits.dtype not in _LOGIT_TYPES:
+    kind = _LOGIT_TYPES.get(logits.dtype)
+    if kind is None:
         raise TypeError(f"expected float16, bfloat16 or float32, got {logits.dtype}")
     N, V = logits.shape
-    for t, n in ((tokens, N), (logprob, N), (entropy, N), (lse, N), (chosen, N), (ids, N * k), (top_logprobs, N * k), (probs, N * k)):
-        if t is not None and t.numel() != n:
-            raise ValueError("a result or the tokens do not have a place for each row (and alternative)")
-    _check(lib().plc_score_tokens(_LOGIT_TYPES[logits.dtype], logits.data_ptr(), logits.stride(0), N, V, scale, _ints_or_none(tokens),
-                                  k, _floats(logprob), _floats(entropy), _floats(lse), _ints_or_none(ids), _floats(top_logprobs),
-                                  _floats(probs), _ints_or_none(chosen), _on_device(ws), ws.numel(), _ints(status), stream),
-           "plc_score_tokens")
+    if tokens is not None:
+        _on(logits.get_device(), tokens)
+        if tokens.numel() != N:
+            raise ValueError("tokens has a number for each row")
+        tokens = _ints(tokens)
+    _check(lib().plc_score_tokens(kind, logits.data_ptr(), logits.stride(0), N, V, scale, tokens, k, *results, stream), "plc_score_tokens")
 
 
 class PrefixTrie:

@@ -41,21 +41,28 @@ class TokenScorer:
             raise ValueError("tokens has a number for each row of logits")
         if not temperature > 0:
             raise ValueError("the temperature is positive")
-        shape = logits.shape[:-1]
+        shape, k, device = logits.shape[:-1], self.k, self.status.device
+        plc._on(logits.get_device(), self.status)
         rows = logits if logits.dim() == 2 else logits.view(-1, self.V) if logits.dim() > 2 else logits.unsqueeze(0)
-        device = logits.device
-        floats = lambda *s: torch.empty(s, dtype=torch.float32, device=device)  # noqa: E731
-        ints = lambda *s: torch.empty(s, dtype=torch.int32, device=device)  # noqa: E731
         logprob = chosen = ids = logprobs = probs = None
-        entropy, lse = floats(*shape), floats(*shape)
-        if tokens is not None:
-            logprob = floats(*shape)
-        if self.k:
-            ids, logprobs, probs = ints(*shape, self.k), floats(*shape, self.k), floats(*shape, self.k)
+        at_logprob = at_chosen = at_ids = at_logprobs = at_probs = None
+        # (results of one shape out of one tensor: each that is made costs as much of the host's time as the kernel's launch half)
+        sums = torch.empty((2 if tokens is None else 3, *shape), dtype=torch.float32, device=device)
+        if tokens is None:
+            entropy, lse = sums.unbind()
+        else:
+            entropy, lse, logprob = sums.unbind()
+            at_logprob = logprob.data_ptr()
+        if k:
+            logprobs = torch.empty((*shape, k), dtype=torch.float32, device=device)
+            probs = torch.empty_like(logprobs)
+            ids = torch.empty((*shape, k), dtype=torch.int32, device=device)
+            at_logprobs, at_probs, at_ids = logprobs.data_ptr(), probs.data_ptr(), ids.data_ptr()
             if tokens is not None:
-                chosen = ints(*shape)
-        plc.plc_score_tokens(rows, 1.0 / temperature, tokens, self.k, logprob, entropy, lse, ids, logprobs, probs, chosen, self.ws,
-                             self.status)
+                chosen = torch.empty_like(tokens)
+                at_chosen = chosen.data_ptr()
+        plc._score_tokens(rows, 1.0 / temperature, tokens, k, at_logprob, entropy.data_ptr(), lse.data_ptr(), at_ids, at_logprobs, at_probs,
+                          at_chosen, self.ws.data_ptr(), self.ws.numel(), self.status.data_ptr())
         return Scores(logprob, entropy, lse, ids, logprobs, probs, chosen)
 
     def check_status(self, where="plc_score_tokens"):
