@@ -3,11 +3,15 @@
 //
 // A lane owns 16 components of a row (8 pairs), and takes them through many heads: the cosines and sines of its pairs are
 // worked out once, by itself, and stay in registers.  With halves that are whole pieces of 16 bytes its components are one piece of
-// each half, interleaved they are two pieces side by side; halves of other widths go component by component.
+// each half, interleaved they are two pieces side by side; halves of other widths go by what they are aligned to, 8, 4 or 2 bytes.
 //
 // The angle in turns, times 2^64, is a whole number; times the position it wraps around exactly as the angle does, so that
 // its upper 32 bits are the fraction of a turn to 2^-32 for any position, where fp32 products of position and frequency are off by
 // 0.06 rad at a million.  Cosine and sine of what is left within an eighth of a turn are sums of their power series.
+//
+// What bounds it: HBM where there is much (4096 rows of 32 layers and 8 heads, 128 components, 1.07 GB in and out, 197 us, 5.4 TB/s; the
+// store that does not rotate 188); in the caches the angles, some 20 instructions for each of a thread's 8 pairs (2048 tokens, 50 MB,
+// 13.5 us); for few rows the host's time (a token's 12 heads: 5.7 us of one launch after the other).
 #include <cmath>
 #include <type_traits>
 
@@ -51,14 +55,55 @@ __device__ __forceinline__ void turn_by(uint32_t f, float *c, float *s) {
   *s = quarter & 2 ? -b : b;
 }
 
-// How a lane's 16 components lie in a row.
+// How a lane's components lie in a row: two runs of up to 8, and the pairs that they make (none: they pass).
 struct Lane {
-  int32_t at[2];   // vectors: its pieces' first components (-1: none)
-  int32_t first, count;  // its pairs, or with count = 0 components that pass
-  uint32_t turned;       // a bit for each of its pairs
+  int32_t at[2], n[2], first, count;
 };
 
-template <class T, bool kStore, bool kVector, bool kStream>
+// A run of n components, in pieces of kWide, which they are a multiple of and aligned as; past the caches (kStream).
+template <int kWide, bool kStream>
+__device__ __forceinline__ uint4 get_run(const uint16_t *from, int32_t n) {
+  if constexpr (kWide == 8) {
+    if (n == 0) return make_uint4(0u, 0u, 0u, 0u);
+    return kStream ? load16_stream(from) : *reinterpret_cast<const uint4 *>(from);
+  } else {
+    typedef uint16_t Piece __attribute__((ext_vector_type(kWide)));
+    typedef uint16_t Eight __attribute__((ext_vector_type(8)));
+    Eight v = {};
+#pragma unroll
+    for (int c = 0; c < 8; c += kWide)
+      if (c < n) {
+        const Piece x = *reinterpret_cast<const Piece *>(from + c);
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) v[c + e] = x[e];
+      }
+    return __builtin_bit_cast(uint4, v);
+  }
+}
+template <int kWide, bool kStream>
+__device__ __forceinline__ void put_run(uint16_t *to, int32_t n, uint4 run) {
+  if constexpr (kWide == 8) {
+    if (n == 0) return;
+    if (kStream) store16_stream(to, run);
+    else *reinterpret_cast<uint4 *>(to) = run;
+  } else {
+    typedef uint16_t Piece __attribute__((ext_vector_type(kWide)));
+    typedef uint16_t Eight __attribute__((ext_vector_type(8)));
+    const Eight v = __builtin_bit_cast(Eight, run);
+#pragma unroll
+    for (int c = 0; c < 8; c += kWide)
+      if (c < n) {
+        Piece x;
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) x[e] = v[c + e];
+        *reinterpret_cast<Piece *>(to + c) = x;
+      }
+  }
+}
+
+// kWide: components that lie aligned together, in halves too (8: interleaved, or halves of whole 16-byte pieces).  kStream: stores past the
+// caches, and with 2 loads too.
+template <class T, bool kStore, int kWide, int kStream>
 __global__ __launch_bounds__(kBlock) void rotate_kernel(RotateArgs a) {
   extern __shared__ int64_t rotate_lds[];  // of a store: [block_rows] in the pool, in the buffer, position; then off i32 [S + 1]
   const PoolView &p = a.p;
@@ -98,16 +143,15 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(RotateArgs a) {
   }
 
   const int32_t half = a.by.r / 2, d = 8 * a.d8, turning = (half + 7) / 8;  // lanes with pairs
-  Lane lane = {{-1, -1}, 8 * j, 0, 0};
-  if (kVector && a.by.interleaved) {
-    lane.at[0] = 16 * j, lane.at[1] = 16 * j + 8 < d ? 16 * j + 8 : -1;
-    lane.count = max(0, min(8, half - 8 * j));
+  Lane lane;
+  if (kWide == 8 && a.by.interleaved) {
+    lane = {{16 * j, 16 * j + 8}, {8, min(8, d - 16 * j - 8)}, 8 * j, max(0, min(8, half - 8 * j))};
   } else if (j < turning) {
-    lane.at[0] = 8 * j, lane.at[1] = 8 * j + half;
-    lane.count = min(8, half - 8 * j);
+    const int32_t n = min(8, half - 8 * j);
+    lane = {{8 * j, 8 * j + half}, {n, n}, 8 * j, n};
   } else {
     const int32_t e = a.by.r + 16 * (j - turning);
-    lane.at[0] = e, lane.at[1] = e + 8 < d ? e + 8 : -1;
+    lane = {{e, e + 8}, {min(8, d - e), max(0, min(8, d - e - 8))}, 0, 0};
   }
   float cs[8], sn[8];
 #pragma unroll
@@ -134,98 +178,58 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(RotateArgs a) {
   const auto turned = [&](int32_t e) { return e < keys || e >= 2 * keys; };
   const int32_t e0 = (int32_t)blockIdx.y * a.slots + slot, step = (int32_t)gridDim.y * a.slots;
 
-  if constexpr (kVector) {
-    typedef T T8 __attribute__((ext_vector_type(8)));
-    constexpr int kBatch = 4;
-    for (int32_t e = e0; e < all; e += kBatch * step) {
-      uint4 in[kBatch][2];
-      uint16_t *to[kBatch];
+  typedef T T8 __attribute__((ext_vector_type(8)));
+  constexpr int kBatch = 4;
+  for (int32_t e = e0; e < all; e += kBatch * step) {
+    uint4 in[kBatch][2];
+    uint16_t *to[kBatch];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int32_t mine = min(e + u * step, all - 1);
-        const uint16_t *from;
-        place(mine, &from, &to[u]);
-        in[u][0] = kStream ? load16_stream(from + lane.at[0]) : *reinterpret_cast<const uint4 *>(from + lane.at[0]);
-        in[u][1] = lane.at[1] < 0 ? make_uint4(0u, 0u, 0u, 0u)
-                   : kStream      ? load16_stream(from + lane.at[1])
-                                  : *reinterpret_cast<const uint4 *>(from + lane.at[1]);
-      }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int32_t mine = e + u * step;
-        if (mine >= all) break;
-        if (turned(mine) && lane.count > 0) {
-          const T8 v0 = __builtin_bit_cast(T8, in[u][0]), v1 = __builtin_bit_cast(T8, in[u][1]);
-          T8 w0 = v0, w1 = v1;
-          if (a.by.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float xa = (float)v0[2 * i], ya = (float)v0[2 * i + 1], xb = (float)v1[2 * i], yb = (float)v1[2 * i + 1];
-              if (i < lane.count) {
-                w0[2 * i] = (T)__builtin_fmaf(xa, cs[i], -(ya * sn[i]));
-                w0[2 * i + 1] = (T)__builtin_fmaf(ya, cs[i], xa * sn[i]);
-              }
-              if (i + 4 < lane.count) {
-                w1[2 * i] = (T)__builtin_fmaf(xb, cs[i + 4], -(yb * sn[i + 4]));
-                w1[2 * i + 1] = (T)__builtin_fmaf(yb, cs[i + 4], xb * sn[i + 4]);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float xa = (float)v0[i], ya = (float)v1[i];
-              w0[i] = (T)__builtin_fmaf(xa, cs[i], -(ya * sn[i]));
-              w1[i] = (T)__builtin_fmaf(ya, cs[i], xa * sn[i]);
-            }
-          }
-          in[u][0] = __builtin_bit_cast(uint4, w0), in[u][1] = __builtin_bit_cast(uint4, w1);
-        }
-        if (kStream) {
-          store16_stream(to[u] + lane.at[0], in[u][0]);
-          if (lane.at[1] >= 0) store16_stream(to[u] + lane.at[1], in[u][1]);
-        } else {
-          *reinterpret_cast<uint4 *>(to[u] + lane.at[0]) = in[u][0];
-          if (lane.at[1] >= 0) *reinterpret_cast<uint4 *>(to[u] + lane.at[1]) = in[u][1];
-        }
-      }
-    }
-  } else {  // halves that are not whole pieces
-    for (int32_t e = e0; e < all; e += step) {
+    for (int u = 0; u < kBatch; ++u) {
       const uint16_t *from;
-      uint16_t *to;
-      place(e, &from, &to);
-      if (lane.count > 0) {
-        uint16_t lo[8], hi[8];
+      place(min(e + u * step, all - 1), &from, &to[u]);
+      in[u][0] = get_run<kWide, kStream == 2>(from + lane.at[0], lane.n[0]);
+      in[u][1] = get_run<kWide, kStream == 2>(from + lane.at[1], lane.n[1]);
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < lane.count) lo[i] = from[lane.at[0] + i], hi[i] = from[lane.at[1] + i];
+    for (int u = 0; u < kBatch; ++u) {
+      const int32_t mine = e + u * step;
+      if (mine >= all) break;
+      if (turned(mine) && lane.count > 0) {
+        const T8 v0 = __builtin_bit_cast(T8, in[u][0]), v1 = __builtin_bit_cast(T8, in[u][1]);
+        T8 w0 = v0, w1 = v1;
+        if (kWide == 8 && a.by.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < lane.count) {
-            if (turned(e)) {
-              const float xa = (float)__builtin_bit_cast(T, lo[i]), ya = (float)__builtin_bit_cast(T, hi[i]);
-              lo[i] = __builtin_bit_cast(uint16_t, (T)__builtin_fmaf(xa, cs[i], -(ya * sn[i])));
-              hi[i] = __builtin_bit_cast(uint16_t, (T)__builtin_fmaf(ya, cs[i], xa * sn[i]));
+          for (int i = 0; i < 4; ++i) {
+            const float xa = (float)v0[2 * i], ya = (float)v0[2 * i + 1], xb = (float)v1[2 * i], yb = (float)v1[2 * i + 1];
+            if (i < lane.count) {
+              w0[2 * i] = (T)__builtin_fmaf(xa, cs[i], -(ya * sn[i]));
+              w0[2 * i + 1] = (T)__builtin_fmaf(ya, cs[i], xa * sn[i]);
             }
-            to[lane.at[0] + i] = lo[i], to[lane.at[1] + i] = hi[i];
+            if (i + 4 < lane.count) {
+              w1[2 * i] = (T)__builtin_fmaf(xb, cs[i + 4], -(yb * sn[i + 4]));
+              w1[2 * i + 1] = (T)__builtin_fmaf(yb, cs[i + 4], xb * sn[i + 4]);
+            }
           }
-      } else {
-        uint16_t w[16];
-        const int32_t n = min(16, d - lane.at[0]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (i < n) w[i] = from[lane.at[0] + i];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (i < n) to[lane.at[0] + i] = w[i];
+          for (int i = 0; i < 8; ++i) {
+            const float xa = (float)v0[i], ya = (float)v1[i];
+            w0[i] = (T)__builtin_fmaf(xa, cs[i], -(ya * sn[i]));
+            w1[i] = (T)__builtin_fmaf(ya, cs[i], xa * sn[i]);
+          }
+        }
+        in[u][0] = __builtin_bit_cast(uint4, w0), in[u][1] = __builtin_bit_cast(uint4, w1);
       }
+      put_run<kWide, kStream != 0>(to[u] + lane.at[0], lane.n[0], in[u][0]);
+      put_run<kWide, kStream != 0>(to[u] + lane.at[1], lane.n[1], in[u][1]);
     }
   }
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kCached = (int64_t)96 << 20;  // bytes moved, in and out, beyond which stores go past the caches
+constexpr int64_t kCached = (int64_t)96 << 20;         // bytes moved, in and out, beyond which stores go past the caches
+constexpr int64_t kLoadedCached = (int64_t)512 << 20;  // beyond which loads do too: what is read may still lie in the last-level cache
 
 bool rotary_valid(const plc_rotary *rot, int32_t d) {
   return rot && aligned(rot->turns, 8) && rot->r >= 2 && rot->r % 2 == 0 && rot->r <= d && d >= 8 && d % 8 == 0 && d <= 2048 &&
@@ -237,32 +241,47 @@ bool strides_ok(const int64_t *stride) {
   return stride && stride[0] >= 0 && stride[0] % 8 == 0 && stride[1] >= 0 && stride[1] % 8 == 0;
 }
 
-template <class T, bool kStore, bool kVector>
+// Four heads to a thread, which its angles are for, while there are two workgroups for each compute unit, else fewer: 2048 tokens with 48
+// heads of keys, values and queries 13.5 us, with up to 8 the same, with one or two at a time 17; 4096 rows of 512 heads 197 us, of
+// up to 8 heads 204, of 16 216.
+template <class T, bool kStore, int kWide>
 int launch_rotate(RotateArgs a, int64_t rows, int64_t heads, hipStream_t st) {
   const int32_t half = a.by.r / 2, d = 8 * a.d8;
-  a.lanes = kVector ? (d + 15) / 16 : (half + 7) / 8 + (d - a.by.r + 15) / 16;
+  a.lanes = kWide == 8 ? (d + 15) / 16 : (half + 7) / 8 + (d - a.by.r + 15) / 16;
   const int32_t units = kBlock / a.lanes;
   a.block_rows = units;
   while (a.block_rows > 1 && a.block_rows / 2 >= rows) a.block_rows /= 2;
   a.slots = units / a.block_rows;
   const int64_t bx = (rows + a.block_rows - 1) / a.block_rows;
   if (bx >= 1 << 24) return PLC_ERR_INVALID;  // (lanes of a launch < 2^32)
-  const int64_t most = (heads + a.slots - 1) / a.slots;
-  int64_t by = (8 * kComputeUnits + bx - 1) / bx;
-  by = by > most ? most : by;
+  int64_t each = 4, by;  // heads of a thread
+  while (true) {
+    by = (heads + each * a.slots - 1) / (each * a.slots);
+    if (each == 1 || bx * by >= 2 * kComputeUnits) break;
+    each /= 2;
+  }
   by = by > 65535 ? 65535 : by;
-  const bool stream = (double)rows * heads * d * 4 > (double)kCached;
+  const double bytes = (double)rows * heads * d * 4;
+  const auto kernel = kWide != 8 || bytes <= (double)kCached ? &rotate_kernel<T, kStore, kWide, 0>
+                      : bytes <= (double)kLoadedCached       ? &rotate_kernel<T, kStore, kWide, kWide == 8 ? 1 : 0>
+                                                             : &rotate_kernel<T, kStore, kWide, kWide == 8 ? 2 : 0>;
   const size_t lds = kStore ? 24 * (size_t)a.block_rows + 4 * (size_t)(a.p.S + 1) : 0;
-  const auto kernel = stream ? &rotate_kernel<T, kStore, kVector, true> : &rotate_kernel<T, kStore, kVector, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)bx, (unsigned)by), dim3(kBlock), lds, st, a);
   return launch_status();
 }
 
+template <class T, bool kStore>
+int rotate(const RotateArgs &a, int64_t rows, int64_t heads, hipStream_t st) {
+  const int32_t half = a.by.r / 2;
+  if (a.by.interleaved || half % 8 == 0) return launch_rotate<T, kStore, 8>(a, rows, heads, st);
+  if (half % 4 == 0) return launch_rotate<T, kStore, 4>(a, rows, heads, st);
+  if (half % 2 == 0) return launch_rotate<T, kStore, 2>(a, rows, heads, st);
+  return launch_rotate<T, kStore, 1>(a, rows, heads, st);
+}
+
 template <bool kStore>
 int rotate(const RotateArgs &a, int32_t type, int64_t rows, int64_t heads, hipStream_t st) {
-  const bool vector = a.by.interleaved || a.by.r % 16 == 0;
-  if (type == PLC_FP16) return vector ? launch_rotate<_Float16, kStore, true>(a, rows, heads, st) : launch_rotate<_Float16, kStore, false>(a, rows, heads, st);
-  return vector ? launch_rotate<__bf16, kStore, true>(a, rows, heads, st) : launch_rotate<__bf16, kStore, false>(a, rows, heads, st);
+  return type == PLC_FP16 ? rotate<_Float16, kStore>(a, rows, heads, st) : rotate<__bf16, kStore>(a, rows, heads, st);
 }
 
 constexpr long double kTwoPi = 6.283185307179586476925286766559005768L;

@@ -179,9 +179,10 @@ def test_a_decoded_cache_into_pages(layout):
         assert same_bits(first[s][0], got_k) and same_bits(first[s][1], got_v)
 
 
-def test_many_rows_past_the_caches():
-    """More than 96 MB, in and out: as in two halves."""
-    L, H, n, d = 16, 8, 1000, 128
+@pytest.mark.parametrize("L,n", [(16, 1000), (32, 2100)])
+def test_many_rows_past_the_caches(L, n):
+    """More than 96 MB, and more than 512 MB, in and out: as a hundred rows at a time."""
+    H, d = 8, 128
     cache, _ = make_cache(torch.bfloat16, d, H, 16, [n], seed=1, L=L)
     k, v = (torch.randn((1, L, H, n, d), device=DEV, dtype=torch.bfloat16) for _ in range(2))
     rotary = Rotary(d)
