@@ -762,7 +762,7 @@ int plc_rotary_frequencies(const plc_rotary_spec *spec /* host */, double *theta
 int plc_rotary_turns(const double *theta /* host */, int32_t pairs, uint64_t *turns /* host */);
 
 /* Rows of a buffer: x, out logical [rows, heads, d] (element strides of row and head, multiples of 8; 16-byte aligned), out may
- * be x, with the same strides; else they must not overlap.  positions i32 [rows].  inverse: turned by -a and divided by the
+ * be x, with the same strides; else they must not overlap.  out's strides, of what there is more than one of, are at least d.  positions i32 [rows].  inverse: turned by -a and divided by the
  * magnitude.  d a multiple of 8, up to 2048; rows * d < 2^35, heads * d < 2^31. */
 int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x, const int64_t *x_stride /* host */,
                int64_t rows, int32_t heads, int32_t d, const int32_t *positions, int32_t inverse, void *out,
@@ -774,7 +774,7 @@ int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x,
  *          plc_pages_evict has thinned out is shorter than what its session has seen).
  *   rel    nullable: i32, one for each row of the buffer (rows, or S * rows); i without.  A drafted tree's nodes: their depths.
  *   q, q_out   nullable, with packed rows: logical [rows->rows, H*G, d], strides (node, head) and alignment as for
- *          plc_attend; q_out may be q, with the same strides.
+ *          plc_attend; q_out may be q, with the same strides; its strides are at least d.
  * Rows that cannot be stored (status) are left alone, in q_out too, and so are rows behind off[S].  d up to 2048,
  * rows (of all sessions) * d < 2^35, layers * H and H * G < 2^29. */
 int plc_rotate_store(const plc_pages *pages /* host */, const plc_rows *rows /* host */, const plc_rotary *rotary /* host */,

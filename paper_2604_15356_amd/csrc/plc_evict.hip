@@ -1,16 +1,18 @@
 // Eviction from the paged cache: in every layer and head by itself the positions that have received most stay, and move
 // together; see include/plc.h.
 //
-// Three kernels, one behind the other, because a session's table, length and counts may not change while others look at them:
+// Kernels one behind the other, because a session's table, length and counts may not change while others look at them:
 //   select_kernel   a workgroup for each session, layer and head: whether the session can be shortened at all, which positions
 //                   stay (a radix selection over the weights as ordered 32-bit keys, 11, 11 and 10 bits), their numbers in
-//                   order, their weights moved together;
-//   move_kernel     their rows moved together, K and V and 128-byte columns of them by workgroups of their own;
+//                   order, their weights moved together, and their rows;
+//   move_kernel     the rows, where there are few heads;
 //   shorten_kernel  lengths, pages.
 // Rows move in place and in order: the row of number j comes from position kept[j] >= j, so that a workgroup that reads the rows
 // of some numbers before it writes any of them needs to look at no other order: what later numbers read lies behind it.
 //
-// What bounds it: HBM for the rows, read once and written once.
+// What bounds it: HBM for the rows, read once and written once (4 sessions of 2048 positions halved in 32 layers of 8 heads, 128
+// components: 1.09 GB in 232 us, 4.7 TB/s; a copy of such a size 5.4); for few the steps of the choice, 7 us for 512 positions: weights,
+// table and counts 2.5, a digit 1.2, the kept ones' numbers 1.
 #include "plc_device.h"
 #include "plc_paged.h"
 
@@ -34,10 +36,64 @@ __device__ __forceinline__ uint32_t key_of(float w) {
   return w != w ? 0xffffffffu : u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 
+constexpr int64_t kLittle = 4096;  // pieces of 16 bytes of a head's K
 constexpr int kBins = 2048;
 // A bin's place: the wavefront that adds them up, 32 in a row to a lane, so reads from all banks.
 __device__ __forceinline__ uint32_t place_of(uint32_t bin) { return (bin & (kBins / 64 - 1)) * 64 + bin / (kBins / 64); }
 constexpr int64_t kCached = (int64_t)96 << 20;  // bytes moved, in and out, beyond which rows go past the caches
+
+// A lane takes 16 bytes of a row (in one column of K's rows, or V's), several rows at a time; all of the workgroup's loads of a round before
+// its first store, and the next round's addresses while they are under way.  kStream: past the caches, in and out.
+constexpr int kMoveBatch = 8;
+template <int kThreads, bool kStream>
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int32_t s, int32_t lh, int32_t of_v, int32_t column, int32_t now) {
+  const PoolView &p = a.p;
+  const int32_t at_once = kThreads / a.pieces, row = (int32_t)threadIdx.x / a.pieces, c = column * a.pieces + (int32_t)threadIdx.x % a.pieces;
+  const bool here = row < at_once && c < p.d8;
+  uint16_t *const base = (of_v ? p.v : p.k) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)min(c, p.d8 - 1) * 8;
+  const int32_t *const kept = a.kept + ((int64_t)s * p.L * p.H + lh) * a.W, *const table = p.table + (int64_t)s * p.M;
+  const int32_t mask = (1 << p.shift) - 1, round = kMoveBatch * at_once, last = now - 1;
+  int32_t from[kMoveBatch], next[kMoveBatch], from_page[kMoveBatch], to_page[kMoveBatch];
+  const auto fetch = [&](int32_t j0) {  // (rows behind the end are read as the last one, and not written)
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) next[u] = kept[min(j0 + u * at_once + row, last)];
+  };
+  const auto fetch_pages = [&](int32_t j0) {
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) {
+      from[u] = next[u];
+      from_page[u] = table[from[u] >> p.shift];
+      to_page[u] = table[min(j0 + u * at_once + row, last) >> p.shift];
+    }
+  };
+  int32_t j0 = a.first;
+  while (j0 + round <= now && kept[j0 + round - 1] == j0 + round - 1) j0 += round;  // nothing has gone before these
+  if (j0 >= now) return;
+  fetch(j0);
+  fetch_pages(j0);
+  for (; j0 < now; j0 += round) {
+    u32x4 v[kMoveBatch];
+    uint16_t *to[kMoveBatch];
+    bool moves[kMoveBatch];
+    if (j0 + round < now) fetch(j0 + round);
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) {
+      const int32_t j = j0 + u * at_once + row;
+      const auto *const at = reinterpret_cast<const u32x4 *>(base + from_page[u] * p.page_s + (from[u] & mask) * p.row_s);
+      v[u] = kStream ? __builtin_nontemporal_load(at) : *at;
+      to[u] = base + to_page[u] * p.page_s + (j & mask) * p.row_s;
+      moves[u] = here && j < now && from[u] != j;
+    }
+    if (j0 + round < now) fetch_pages(j0 + round);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u)
+      if (moves[u]) {
+        if (kStream) __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4 *>(to[u]));
+        else *reinterpret_cast<u32x4 *>(to[u]) = v[u];
+      }
+  }
+}
 
 // Runs of four positions that a thread holds, at a distance of the workgroup's: 16 positions for each thread are looked at without
 // being read again.
@@ -62,7 +118,8 @@ struct Held {
   }
 };
 
-template <int kThreads>
+// kMove: what moves with the choice; 0: the rows stay for kernels of their own; 1, 2: here, 2 past the caches.
+template <int kThreads, int kMove>
 __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / 64;
   using Block = Held<kThreads>;
@@ -198,65 +255,17 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
       }
       above += total & 0xffffu, equal += total >> 16;
     }
-    __syncthreads();  // `meet` is written again
+    __syncthreads();  // `meet` is written again; and all of `kept` is there
   }
+  if constexpr (kMove != 0)
+    for (int32_t i = 0; i < 2 * a.columns; ++i) move_rows<kThreads, kMove == 2>(a, s, lh, i / a.columns, i % a.columns, (int32_t)now);
 }
 
-// A lane takes 16 bytes of a row, several rows at a time; all of the workgroup's loads of a round before its first store, and the next
-// round's addresses while they are under way.  kStream: past the caches, in and out.
-constexpr int kMoveBatch = 8;
+// The rows of a session, layer and head where they are moved by workgroups of their own: K and V, and 128-byte columns of them.
 template <bool kStream>
 __global__ __launch_bounds__(kBlock) void move_kernel(EvictArgs a) {
-  const PoolView &p = a.p;
-  const int32_t s = (int32_t)blockIdx.y, now = a.now[s];
-  if (now < 0) return;
-  const int32_t heads = p.L * p.H, unit = (int32_t)blockIdx.x;
-  const int32_t column = unit % a.columns, of_v = unit / a.columns & 1, lh = unit / (2 * a.columns);
-  const int32_t at_once = kBlock / a.pieces, row = (int32_t)threadIdx.x / a.pieces, c = column * a.pieces + (int32_t)threadIdx.x % a.pieces;
-  const bool here = row < at_once && c < p.d8;
-  uint16_t *const base = (of_v ? p.v : p.k) + (lh / p.H) * p.layer_s + (lh % p.H) * p.head_s + (int64_t)min(c, p.d8 - 1) * 8;
-  const int32_t *const kept = a.kept + ((int64_t)s * heads + lh) * a.W, *const table = p.table + (int64_t)s * p.M;
-  const int32_t mask = (1 << p.shift) - 1, round = kMoveBatch * at_once, last = now - 1;
-  int32_t from[kMoveBatch], next[kMoveBatch], from_page[kMoveBatch], to_page[kMoveBatch];
-  const auto fetch = [&](int32_t j0) {  // (rows behind the end are read as the last one, and not written)
-#pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u) next[u] = kept[min(j0 + u * at_once + row, last)];
-  };
-  const auto fetch_pages = [&](int32_t j0) {
-#pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u) {
-      from[u] = next[u];
-      from_page[u] = table[from[u] >> p.shift];
-      to_page[u] = table[min(j0 + u * at_once + row, last) >> p.shift];
-    }
-  };
-  int32_t j0 = a.first;
-  while (j0 + round <= now && kept[j0 + round - 1] == j0 + round - 1) j0 += round;  // nothing has gone before these
-  if (j0 >= now) return;
-  fetch(j0);
-  fetch_pages(j0);
-  for (; j0 < now; j0 += round) {
-    u32x4 v[kMoveBatch];
-    uint16_t *to[kMoveBatch];
-    bool moves[kMoveBatch];
-    if (j0 + round < now) fetch(j0 + round);
-#pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u) {
-      const int32_t j = j0 + u * at_once + row;
-      const auto *const at = reinterpret_cast<const u32x4 *>(base + from_page[u] * p.page_s + (from[u] & mask) * p.row_s);
-      v[u] = kStream ? __builtin_nontemporal_load(at) : *at;
-      to[u] = base + to_page[u] * p.page_s + (j & mask) * p.row_s;
-      moves[u] = here && j < now && from[u] != j;
-    }
-    if (j0 + round < now) fetch_pages(j0 + round);
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u)
-      if (moves[u]) {
-        if (kStream) __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4 *>(to[u]));
-        else *reinterpret_cast<u32x4 *>(to[u]) = v[u];
-      }
-  }
+  const int32_t s = (int32_t)blockIdx.y, now = a.now[s], unit = (int32_t)blockIdx.x;
+  if (now >= 0) move_rows<kBlock, kStream>(a, s, unit / (2 * a.columns), unit / a.columns & 1, unit % a.columns, now);
 }
 
 __global__ __launch_bounds__(kBlock) void shorten_kernel(EvictArgs a) {
@@ -286,15 +295,20 @@ extern "C" int plc_pages_evict(const plc_pages *pages, const int32_t *keep, int3
   const int64_t heads = (int64_t)a.p.L * a.p.H;
   if (heads >= 1 << 22 || heads * pages->d >= 1 << 29) return PLC_ERR_INVALID;  // (lanes of a launch < 2^32)
   const dim3 grid((unsigned)heads, (unsigned)a.p.S);
-  // Whole rows where there are heads enough to fill the chip (4 sessions, 32 layers, 8 heads, 2048 positions to half: 244 against 250 us; 64
-  // sessions of 200: 452 against 474), else lines of 128 bytes, a workgroup each.
+  // Where there are sessions and heads enough for all compute units, or little to move, a workgroup moves what it has chosen, whole rows at a
+  // time; else K and V and their lines of 128 bytes have workgroups of their own.  (32 layers and 8 heads, 128 components, halved: 64 sessions of 200
+  // positions 337 against 389 us, a session of 8000 228 against 235; of 8 layers, 4 sessions of 2000 65 against 70; of 4, 53 against 42.)
   const int64_t rows = heads * a.p.S;
-  a.pieces = a.p.d8 > kBlock ? kBlock : a.p.d8 % 16 == 0 && rows >= 2 * kComputeUnits ? 16 : a.p.d8 % 8 == 0 ? 8 : a.p.d8;
-  a.columns = (a.p.d8 + a.pieces - 1) / a.pieces;
+  const bool together = rows >= kComputeUnits || (int64_t)W * a.p.d8 <= kLittle;
   const bool past = (double)rows * W * a.p.d8 * 64 > (double)kCached;  // of both halves, in and out
-  if (max_len <= 4096) hipLaunchKernelGGL(select_kernel<256>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(select_kernel<1024>, grid, dim3(1024), 0, st, a);
-  hipLaunchKernelGGL(past ? &move_kernel<true> : &move_kernel<false>, dim3((unsigned)(heads * 2 * a.columns), (unsigned)a.p.S), dim3(kBlock), 0, st, a);
+  a.pieces = a.p.d8 > kBlock ? kBlock : !together && a.p.d8 % 8 == 0 ? 8 : a.p.d8;
+  a.columns = (a.p.d8 + a.pieces - 1) / a.pieces;
+  const auto chosen = max_len <= 4096 ? (!together ? &select_kernel<256, 0> : past ? &select_kernel<256, 2> : &select_kernel<256, 1>)
+                                      : (!together ? &select_kernel<1024, 0> : past ? &select_kernel<1024, 2> : &select_kernel<1024, 1>);
+  hipLaunchKernelGGL(chosen, grid, dim3(max_len <= 4096 ? 256 : 1024), 0, st, a);
+  if (!together)
+    hipLaunchKernelGGL(past ? &move_kernel<true> : &move_kernel<false>, dim3((unsigned)(heads * 2 * a.columns), (unsigned)a.p.S),
+                       dim3(kBlock), 0, st, a);
   hipLaunchKernelGGL(shorten_kernel, dim3((unsigned)a.p.S), dim3(kBlock), 0, st, a);
   return launch_status();
 }

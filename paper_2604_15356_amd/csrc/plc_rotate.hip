@@ -244,6 +244,11 @@ bool strides_ok(const int64_t *stride) {
 // Four heads to a thread, which its angles are for, while there are two workgroups for each compute unit, else fewer: 2048 tokens with 48
 // heads of keys, values and queries 13.5 us, with up to 8 the same, with one or two at a time 17; 4096 rows of 512 heads 197 us, of
 // up to 8 heads 204, of 16 216.
+// (Rows that are written may not lie on each other.)
+bool strides_out_ok(const int64_t *stride, int64_t rows, int64_t heads, int32_t d) {
+  return strides_ok(stride) && (rows <= 1 || stride[0] >= d) && (heads <= 1 || stride[1] >= d);
+}
+
 template <class T, bool kStore, int kWide>
 int launch_rotate(RotateArgs a, int64_t rows, int64_t heads, hipStream_t st) {
   const int32_t half = a.by.r / 2, d = 8 * a.d8;
@@ -338,7 +343,7 @@ extern "C" int plc_rotary_turns(const double *theta, int32_t pairs, uint64_t *tu
 extern "C" int plc_rotate(const plc_rotary *rotary, int32_t type, const void *x, const int64_t *x_stride, int64_t rows,
                           int32_t heads, int32_t d, const int32_t *positions, int32_t inverse, void *out,
                           const int64_t *out_stride, void *stream) {
-  if (!rotary_valid(rotary, d) || (type != PLC_FP16 && type != PLC_BF16) || !strides_ok(x_stride) || !strides_ok(out_stride) ||
+  if (!rotary_valid(rotary, d) || (type != PLC_FP16 && type != PLC_BF16) || !strides_ok(x_stride) || !strides_out_ok(out_stride, rows, heads, d) ||
       rows < 0 || rows > INT32_MAX || heads < 1 || (int64_t)heads * d > INT32_MAX || (inverse != 0 && inverse != 1))
     return PLC_ERR_INVALID;
   if (x == out && (x_stride[0] != out_stride[0] || x_stride[1] != out_stride[1])) return PLC_ERR_INVALID;
@@ -363,7 +368,7 @@ extern "C" int plc_rotate_store(const plc_pages *pages, const plc_rows *rows, co
       (int64_t)rows->layers * pages->H >= 1 << 29)
     return PLC_ERR_INVALID;
   if ((q == nullptr) != (q_out == nullptr)) return PLC_ERR_INVALID;
-  if (q && (!rows->packed || !strides_ok(q_stride) || !strides_ok(q_out_stride) || G < 1 || (int64_t)pages->H * G >= 1 << 29 ||
+  if (q && (!rows->packed || !strides_ok(q_stride) || G < 1 || !strides_out_ok(q_out_stride, rows->rows, (int64_t)pages->H * G, pages->d) || (int64_t)pages->H * G >= 1 << 29 ||
             (q == q_out && (q_stride[0] != q_out_stride[0] || q_stride[1] != q_out_stride[1]))))
     return PLC_ERR_INVALID;
   if (rows->rows == 0) return PLC_OK;

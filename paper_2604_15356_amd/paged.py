@@ -101,6 +101,8 @@ class PagedKVCache:
         k, v, layer = self._rows(k, v, layer)
         if rotary.d != self.d:
             raise ValueError(f"a rotation of {rotary.d} components, rows of {self.d}")
+        if rotary.turns.device != self.device:
+            raise ValueError("the rotation is on another device than the cache")
         if q is not None and q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         plc.plc_rotate_store(self.pages, rotary.rotary, self._per_session(off, self.S + 1, "off"), base, rel, k, v, layer, q,
@@ -166,10 +168,9 @@ class PagedKVCache:
         if self._weights_known is None or self._weights_known[0] != layout:
             if w.device != self.device:
                 raise ValueError("the weights are on another device than the cache")
-            self._weights_known = layout, plc.make_weights(self.pages, w)
-        view = self._weights_known[1]
-        view.w = w.data_ptr()
-        return view
+            view = plc.make_weights(self.pages, w)
+            self._weights_known = layout, view.stride, view.width
+        return plc.plc_weights(w.data_ptr(), *self._weights_known[1:])
 
     def add_weights(self, q, off, lse, weights, decay=1.0, layer=0, scale=None, max_nodes=None, max_len=None):
         """Adds to weights (make_weights) what `layer`'s positions receive from the sessions' last off[s+1] - off[s] positions, a

@@ -34,6 +34,8 @@ class Rotary:
         may be x."""
         if x.dim() != 3 or x.shape[2] != self.d:
             raise ValueError(f"rows are [rows, heads, {self.d}]")
+        if x.device != self.turns.device:
+            raise ValueError("the rows are on another device than the rotation")
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
         plc.plc_rotate(self.rotary, x, positions, inverse, out)

@@ -81,7 +81,8 @@ def test_rotations_that_are_refused(over):
 @pytest.mark.parametrize("over", [
     dict(type=2), dict(type=-1), dict(x=None), dict(x=ODD), dict(x=C.c_void_p(4104)), dict(out=None), dict(out=C.c_void_p(8200)), dict(pos=None), dict(pos=ODD),
     dict(xs=(60, 64)), dict(xs=(-8, 64)), dict(os=(128, 4)), dict(n=-1), dict(n=1 << 31), dict(heads=0), dict(heads=1 << 26), dict(d=60), dict(d=2056),
-    dict(inverse=2), dict(out=P, os=(256, 64)), dict(out=P, os=(128, 128))])
+    dict(inverse=2), dict(out=P, os=(256, 64)), dict(out=P, os=(128, 128)),
+    dict(os=(0, 64)), dict(os=(128, 56))])
 def test_rows_that_are_refused(over):
     assert rotate(**over) == INVALID
 
@@ -102,7 +103,7 @@ def store(g=None, r=None, y=None, type=0, off=P, base=None, rel=None, k=P, v=P, 
     dict(g=pages(k=None)), dict(g=pages(B=8)), dict(g=pages(d=2056, stride3=2056)), dict(r=rows(layer=1)), dict(r=rows(layers=0)), dict(r=rows(packed=2)),
     dict(r=rows(rows=-1)), dict(r=rows(stride1=4)), dict(r=rows(packed=0)), dict(type=2), dict(off=None), dict(off=ODD), dict(base=ODD), dict(rel=ODD),
     dict(k=None), dict(v=ODD), dict(q=None), dict(qo=None), dict(q=C.c_void_p(4104)), dict(qo=ODD), dict(qs=(4, 64)), dict(qos=(256, -8)), dict(G=0),
-    dict(G=1 << 29), dict(qo=P, qos=(512, 64)), dict(status=None)])
+    dict(G=1 << 29), dict(qo=P, qos=(512, 64)), dict(qos=(0, 64)), dict(qos=(256, 0)), dict(status=None)])
 def test_stores_that_are_refused(over):
     assert store(**over) == INVALID
 
