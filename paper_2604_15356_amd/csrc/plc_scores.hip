@@ -13,9 +13,11 @@
 // Keys are 64 bits, the logit as an ordered whole number over the token's complement: no two are equal, so that the
 // result does not depend on the order they came in.
 //
-// What bounds it: HBM for many rows (4096 rows of 50,016 bf16 logits, 410 MB, k = 8: 83 us, 4.9 TB/s; k = 0: 77 us, k = 32: 87), a
-// workgroup for each; for few the host's time, and behind that the stages of one workgroup (a row of 50,016, k = 4: 9.4 us, of which the
-// load 2, sums and maxima 3, the k largest 3).  Long rows, where they are few, are cut into parts that a second kernel joins.
+// What bounds it: HBM for many rows (4096 rows of 50,016 bf16 logits, 410 MB, k = 8: 83 us, 4.9 TB/s; k = 0 78 us, k = 32 85), a
+// workgroup for each; for few the host's time, and behind that the steps of one workgroup, one behind the other (a row of 50,016, k = 4: 9.3
+// us).  Long rows, where they are few, are cut into parts that a second kernel joins.  (A workgroup of 1024 threads for a row 12.2 us; the
+// bound from 256 maxima 95 us for the 4096 rows; all that the threads with such maxima have seen read again 111 us for k = 32, where its scattered
+// lines are as many as the row's; a bound from the first 8192 logits, and each piece looked at against it, 150.)
 #include <type_traits>
 
 #include "plc_device.h"

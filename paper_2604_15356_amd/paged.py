@@ -3,8 +3,9 @@ plc_attend, as codec.py is around the coding path.
 
 A cache that codec.py has decoded is put to work here: `store` takes the decoder's [S, L, H, n, d], `fork` lets sessions go
 on from each other's prefix (what PrefixTrie.best_match found, the beams of a search), `extend` makes room for the tokens of
-a step or for a tree of drafted ones, `attend` computes their attention, `accept` keeps the verified nodes, and `load` gives
-the rows back for the encoder.  Everything works in place, in the order of the current stream, without synchronising;
+a step or for a tree of drafted ones, `store_rotated` turns their keys and queries to their positions, `attend` computes their
+attention, `accept` keeps the verified nodes, `add_weights` and `evict` keep a cache that may not grow to the positions that attention goes to,
+and `load` gives the rows back for the encoder.  Everything works in place, in the order of the current stream, without synchronising;
 errors in the data show in `check_status`.  A cache is used from one stream at a time: its workspaces are its own.
 examples/speculative_decoding.py has all of it in a serving loop."""
 from __future__ import annotations
@@ -190,7 +191,8 @@ class PagedKVCache:
     def evict(self, keep, weights, kept=None, first=0, last=0, max_len=None):
         """Every session of more than keep[s] positions (int32 [S]) is shortened to that, in each layer and head to its first and
         last positions and those with the largest weights, which move along.  Returns kept, int32 [S, L, H, W]: the positions
-        that stayed, in front; given, its W bounds keep and shorter sessions.  The pages from position `first` on have to be the sessions' own."""
+        that stayed, in front; W is at least what a session has afterwards (default: max_len).  The pages from position `first` on have to be
+        the sessions' own: what others share can stay as the first positions.  max_len: no session has more (default: what the table holds)."""
         self._per_session(keep, self.S, "keep")
         max_len = self.M * self.B if max_len is None else max_len
         if kept is None:

@@ -107,6 +107,26 @@ def test_long_sessions(n, keep, max_len):
     check(cache, random_weights(cache, n + 1), [max(1, keep // 2), 60], max_len=max_len, last=min(1, keep // 2))
 
 
+@pytest.mark.parametrize("L,H,n,max_len", [(8, 8, 900, 900), (8, 40, 400, 5000), (2, 3, 6000, 6000)])
+def test_rows_past_the_caches(L, H, n, max_len):
+    """More than 96 MB in and out, moved by the workgroups that choose and by others: sampled heads, and all rows against what `kept` says."""
+    cache, rows = make_cache(torch.float16, 256, H, 64, [n, n], seed=n, L=L)
+    weights = random_weights(cache, n)
+    w0, k0, v0 = weights.clone(), *(x.view(2, n, L, H, 256).clone() for x in rows)
+    kept = cache.evict(ints([n // 2, n - 1]), weights, first=2, last=5, max_len=max_len)
+    cache.check_status()
+    for s, now in enumerate((n // 2, n - 1)):
+        got_k, got_v = rows_of(cache, s)
+        assert got_k.shape[0] == now
+        idx = kept[s, :, :, :now].long()
+        for layer in range(L):
+            at = idx[layer].t()[..., None].expand(now, H, 256)
+            assert same_bits(got_k[:, layer], torch.gather(k0[s, :, layer], 0, at)) and same_bits(got_v[:, layer], torch.gather(v0[s, :, layer], 0, at))
+        for layer, h in ((0, 0), (L - 1, H - 1), (L // 2, 1)):
+            assert kept[s, layer, h, :now].tolist() == chosen(w0[s, layer, h, :n].tolist(), now, 2, 5)
+        assert torch.equal(weights[s, :, :, :now], torch.gather(w0[s], 2, idx))
+
+
 def test_borders_of_what_may_stay():
     lens = [64, 64, 64, 64, 64]
     cache, _ = make_cache(torch.float16, 32, 2, 16, lens, seed=1)

@@ -133,6 +133,20 @@ def test_ties_and_orders(dtype, N):
 
 
 @TYPES
+@pytest.mark.parametrize("N", [2, 520])
+@pytest.mark.parametrize("V", [20000, 8192, 140000])
+def test_many_large_logits_with_few_threads(dtype, N, V):
+    """Thousands of candidates: 31 fours of threads see nothing but large logits, one more a few that are smaller, the others none."""
+    at = torch.arange(V, device=DEV) // (4 if dtype == torch.float32 else 8) % 256 // 4  # the four that reads a logit
+    noise = torch.rand((2, V), device=DEV)
+    x = torch.where(at < 31, 5 + 2 * noise, torch.where(at == 31, noise, torch.full_like(noise, -1.0)))
+    x = x.to(dtype)[torch.arange(N, device=DEV) % 2].contiguous()
+    tokens = x.float().argmax(1).to(torch.int32)
+    for k in (32, 20):
+        check(x, k, tokens)
+
+
+@TYPES
 @pytest.mark.parametrize("N", [3, 520])
 def test_masked_tokens(dtype, N):
     x, tokens = draw(N, 9999, dtype)

@@ -92,6 +92,14 @@ def test_many_rows(lens, counts, G, H):
     run(torch.float16, 96, G, H, 32, lens, counts, seed=sum(counts), decay=0.25)
 
 
+@BOTH
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_more_tiles_than_a_wavefront_takes(dtype, d):
+    """So many sessions and heads that a wavefront takes several tiles: lengths that end in each of them."""
+    lens = [500, 1, 33, 64, 65, 127, 128, 129, 200, 257, 300, 512] * 8
+    run(dtype, d, 1, 64 if d < 256 else 32, 16, lens, [1] * len(lens), seed=d)
+
+
 def test_a_layer_of_several_and_rows_with_gaps():
     run(torch.float16, 64, 2, 3, 16, [77, 20], [5, 2], seed=8, L=3, layer=1, layout="gaps")
     run(torch.bfloat16, 72, 4, 2, 64, [500, 20], [64, 2], seed=9, L=2, layer=1, layout="gaps", decay=0.0)
