@@ -373,7 +373,7 @@ __global__ __launch_bounds__(kBlock) void score_kernel(ScoreArgs a) {
     for (int32_t r0 = q0; r0 < q1; r0 += kBlock) {
       const int32_t j = r0 + (int32_t)threadIdx.x;
       const uint64_t bound = list.bound;
-      if (j < q1) take(row.load(j), j, bound, logit_of(bound));
+      if (j < q1) take(row.load(j), j, bound, bound ? logit_of(bound) : -__builtin_inff());
       __syncthreads();  // (nobody adds to the list before everybody has read how long it is)
       const bool full = list.count > Shape::kLimit;
       __syncthreads();

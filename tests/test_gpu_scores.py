@@ -166,10 +166,10 @@ def test_masked_tokens(dtype, N):
 
 
 @TYPES
-@pytest.mark.parametrize("N", [2, 600])
-def test_logits_of_any_size(dtype, N):
-    """Nothing but the type's lowest value; the largest ones; differences that overflow where they are scaled."""
-    V = 8200
+@pytest.mark.parametrize("N,V", [(2, 8200), (600, 8200), (2, 140000)])
+def test_logits_of_any_size(dtype, N, V):
+    """Nothing but the type's lowest value; the largest ones; differences that overflow where they are scaled.  Whole rows, and
+    rows in parts, of which one has a larger logit than the others, and one none."""
     most = torch.finfo(dtype).max
     for value in (-most, most, most / 2):
         x = torch.full((N, V), value, device=DEV, dtype=dtype)
@@ -177,12 +177,17 @@ def test_logits_of_any_size(dtype, N):
         got = TokenScorer(V, 4).score(x, torch.full((N,), 77, dtype=torch.int32, device=DEV))
         even = math.log(V)
         assert abs(float(got.entropy[0]) - even) < 1e-5 and abs(float(got.logprob[0]) + even) < 1e-5
-        assert abs(float(got.lse[0].double()) - float(x[0, 0].double())) <= max(10.0, 1e-6 * float(x[0, 0].abs().double()))
+        # V equal logits: lse = x + log V, which is 11.85 for 140000 of them, and its sum one fp32 rounding, 2^-24 of it
+        assert abs(float(got.lse[0].double()) - (float(x[0, 0].double()) + even)) <= 1e-5 + 2.0 ** -23 * float(x[0, 0].abs().double())
         assert got.ids[0].tolist() == [0, 1, 2, 3] and got.chosen[0] == -1
         if value > 0:
             assert got.logprob[1] < -1e3 and abs(float(got.entropy[1]) - math.log(V - 1)) < 1e-5
     x, tokens = draw(N, V, dtype, spread=1e4)
     check(x, 8, tokens)
+    x = torch.full((N, V), -most, device=DEV, dtype=dtype)
+    x[:, V // 2:V // 2 + 100] = draw(N, 100, dtype)[0]
+    x[:, : V // 3] = -math.inf
+    check(x, 32, torch.full((N,), V // 2 + 50, dtype=torch.int32, device=DEV))
 
 
 @TYPES
