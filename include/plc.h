@@ -762,8 +762,9 @@ int plc_rotary_frequencies(const plc_rotary_spec *spec /* host */, double *theta
 int plc_rotary_turns(const double *theta /* host */, int32_t pairs, uint64_t *turns /* host */);
 
 /* Rows of a buffer: x, out logical [rows, heads, d] (element strides of row and head, multiples of 8; 16-byte aligned), out may
- * be x, with the same strides; else they must not overlap.  out's strides, of what there is more than one of, are at least d.  positions i32 [rows].  inverse: turned by -a and divided by the
- * magnitude.  d a multiple of 8, up to 2048; rows * d < 2^35, heads * d < 2^31. */
+ * be x, with the same strides; else they must not overlap.  out's rows lie apart from each other, a row's heads within the
+ * distance of its rows or a head's rows within that of its heads.  positions i32 [rows].  inverse: turned by -a and divided by
+ * the magnitude.  d a multiple of 8, up to 2048; rows * d < 2^35, heads * d < 2^31. */
 int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x, const int64_t *x_stride /* host */,
                int64_t rows, int32_t heads, int32_t d, const int32_t *positions, int32_t inverse, void *out,
                const int64_t *out_stride /* host */, void *stream);
@@ -774,7 +775,7 @@ int plc_rotate(const plc_rotary *rotary /* host */, int32_t type, const void *x,
  *          plc_pages_evict has thinned out is shorter than what its session has seen).
  *   rel    nullable: i32, one for each row of the buffer (rows, or S * rows); i without.  A drafted tree's nodes: their depths.
  *   q, q_out   nullable, with packed rows: logical [rows->rows, H*G, d], strides (node, head) and alignment as for
- *          plc_attend; q_out may be q, with the same strides; its strides are at least d.
+ *          plc_attend; q_out may be q, with the same strides; its rows lie apart as plc_rotate's out.
  * Rows that cannot be stored (status) are left alone, in q_out too, and so are rows behind off[S].  d up to 2048,
  * rows (of all sessions) * d < 2^35, layers * H and H * G < 2^29. */
 int plc_rotate_store(const plc_pages *pages /* host */, const plc_rows *rows /* host */, const plc_rotary *rotary /* host */,
@@ -788,8 +789,8 @@ int plc_rotate_store(const plc_pages *pages /* host */, const plc_rows *rows /* 
  * session, what the rows of a call give it; plc_pages_evict keeps the positions that have received most.
  *
  *   weights   fp32, logical [S, L, H, width] through `stride` (of session, layer, head; positions are contiguous): what
- *             position p of a session has received in a layer and KV head.  16-byte aligned; strides and width multiples of 4, strides
- *             (of what there is more than one of) at least the width.
+ *             position p of a session has received in a layer and KV head.  16-byte aligned; strides and width multiples of 4.
+ *             No two lie on each other: in the order of their strides, each reaches past what those before it span.
  */
 typedef struct plc_weights {
   float *w;

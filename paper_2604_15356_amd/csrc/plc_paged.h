@@ -69,13 +69,30 @@ struct WeightsView {
   int64_t sess_s, layer_s, head_s, width;
 };
 
+// Whether runs of `extent` elements lie apart from each other, of which there are count[i] at a stride[i]: from the smallest stride
+// to the largest each reaches past what the ones before it span.
+template <int kDims>
+inline bool lie_apart(const int64_t (&count)[kDims], const int64_t *stride, int64_t extent) {
+  __int128 span = extent;
+  bool done[kDims] = {};
+  for (int step = 0; step < kDims; ++step) {
+    int next = -1;
+    for (int i = 0; i < kDims; ++i)
+      if (!done[i] && (next < 0 || stride[i] < stride[next])) next = count[i] > 1 ? i : next;
+    if (next < 0) return true;
+    if (stride[next] < span) return false;
+    span += (__int128)(count[next] - 1) * stride[next];
+    done[next] = true;
+  }
+  return true;
+}
+
 // (Sessions, layers and heads each have weights of their own: workgroups rewrite them side by side.)
 inline bool weights_valid(const plc_pages *p, const plc_weights *w) {
   if (!w || !aligned(w->w, 16) || w->width < 1 || w->width % 4) return false;
-  const int32_t count[3] = {p->S, p->L, p->H};
   for (int i = 0; i < 3; ++i)
-    if (w->stride[i] % 4 || w->stride[i] < (count[i] > 1 ? w->width : 0)) return false;
-  return true;
+    if (w->stride[i] % 4 || w->stride[i] < 0) return false;
+  return lie_apart<3>({p->S, p->L, p->H}, w->stride, w->width);
 }
 
 inline WeightsView weights_view(const plc_weights *w) {

@@ -241,14 +241,14 @@ bool strides_ok(const int64_t *stride) {
   return stride && stride[0] >= 0 && stride[0] % 8 == 0 && stride[1] >= 0 && stride[1] % 8 == 0;
 }
 
+// (Rows that are written may not lie on each other.)
+bool strides_out_ok(const int64_t *stride, int64_t rows, int64_t heads, int32_t d) {
+  return strides_ok(stride) && lie_apart<2>({rows, heads}, stride, d);
+}
+
 // Four heads to a thread, which its angles are for, while there are two workgroups for each compute unit, else fewer: 2048 tokens with 48
 // heads of keys, values and queries 13.5 us, with up to 8 the same, with one or two at a time 17; 4096 rows of 512 heads 197 us, of
 // up to 8 heads 204, of 16 216.
-// (Rows that are written may not lie on each other.)
-bool strides_out_ok(const int64_t *stride, int64_t rows, int64_t heads, int32_t d) {
-  return strides_ok(stride) && (rows <= 1 || stride[0] >= d) && (heads <= 1 || stride[1] >= d);
-}
-
 template <class T, bool kStore, int kWide>
 int launch_rotate(RotateArgs a, int64_t rows, int64_t heads, hipStream_t st) {
   const int32_t half = a.by.r / 2, d = 8 * a.d8;

@@ -125,6 +125,20 @@ def test_weighings_that_are_refused(over):
     assert weigh(**over) == INVALID
 
 
+# Each stride for itself is as large as what it steps over, and together they meet.
+@pytest.mark.parametrize("over", [dict(stride0=128, stride1=128), dict(stride0=64, stride1=192), dict(stride0=128, stride1=256, stride2=256),
+                                  dict(stride0=192, stride1=128), dict(stride0=1 << 62, stride1=64)])
+def test_weights_that_lie_on_each_other_are_refused(over):
+    assert weigh(w=weights(**over)) == INVALID
+    assert evict(w=weights(**over)) == INVALID
+
+
+@pytest.mark.parametrize("strides", [(64, 64), (128, 192), (192, 128), (64, 256)])
+def test_outputs_that_lie_on_each_other_are_refused(strides):
+    assert rotate(heads=3, os=strides) == INVALID
+    assert store(qos=strides) == INVALID
+
+
 def evict(g=None, keep=P, first=1, last=2, w=None, kept=P, W=30, max_len=64, ws=P, ws_bytes=BIG, status=P):
     return plc.lib().plc_pages_evict(C.byref(g or pages()), keep, first, last, C.byref(w or weights()), kept, W, max_len, ws, ws_bytes, status, None)
 
