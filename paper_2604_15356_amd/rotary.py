@@ -18,13 +18,15 @@ class Rotary:
 
     def __init__(self, d, r=None, base=10000.0, interleaved=False, scaling="none", factor=1.0, low=1.0, high=2.0, trained=1,
                  magnitude=1.0, theta=None, device="cuda"):
-        if theta is None:
+        if theta is not None:
+            theta = [float(t) for t in theta]
+            if r is not None and r != 2 * len(theta):
+                raise ValueError("theta has a number for each of r / 2 pairs")
+        else:
             theta = plc.plc_rotary_frequencies(d if r is None else r, scaling, base, factor, low, high, trained)
-        elif r is not None and r != 2 * len(theta):
-            raise ValueError("theta has a number for each of r / 2 pairs")
         if not theta or 2 * len(theta) > d:
             raise ValueError(f"{2 * len(theta)} of {d} components cannot be rotated")
-        self.d, self.theta, self.interleaved, self.magnitude = d, list(theta), bool(interleaved), float(magnitude)
+        self.d, self.theta, self.interleaved, self.magnitude = d, theta, bool(interleaved), float(magnitude)
         signed = [t - (1 << 64) if t >> 63 else t for t in plc.plc_rotary_turns(theta)]
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
         self.rotary = plc.make_rotary(self.turns, interleaved, magnitude)

@@ -74,6 +74,27 @@ def test_far_positions(dtype):
         close(rotary.rotate(x, ints(positions)), want, size, dtype)
 
 
+@pytest.mark.parametrize("kind", ["list", "tensor", "generator"])
+def test_angles_that_are_given(kind):
+    """Whatever holds the numbers, they are taken once."""
+    numbers = [0.5 ** i for i in range(8)]
+    theta = {"list": numbers, "tensor": torch.tensor(numbers), "generator": (t for t in numbers)}[kind]
+    rotary = Rotary(32, r=16, theta=theta)
+    assert rotary.theta == numbers
+    x = torch.randn((2, 3, 32), device=DEV).to(torch.float16)
+    assert same_bits(rotary.rotate(x, ints([7, 100])), Rotary(32, theta=numbers).rotate(x, ints([7, 100])))
+
+
+def test_outputs_that_are_parts_of_others():
+    """Heads outermost, and rows among other rows: apart from each other, whichever stride is the larger."""
+    rotary, positions = Rotary(64), [5, 0, 77, 1 << 20]
+    x = torch.randn((4, 3, 64), device=DEV).to(torch.bfloat16)
+    want = rotary.rotate(x, ints(positions))
+    for out in (torch.zeros((3, 4, 64), device=DEV, dtype=x.dtype).transpose(0, 1),
+                torch.zeros((4, 5, 72), device=DEV, dtype=x.dtype)[:, 1:4, :64]):
+        assert same_bits(rotary.rotate(x, ints(positions), out=out), want)
+
+
 def test_every_eighth_of_a_turn():
     """Angles on both sides of where cosine and sine change their series."""
     theta = [2 * math.pi * (i / 64 + e) for i in range(64) for e in (-1e-9, 0.0, 1e-9)]
