@@ -13,7 +13,8 @@
 // sessions of 512 tokens after 8192 positions 335 us, 0.84 PFLOP/s, where the matrix cores are busy 0.39 of the time and vector instructions
 // are issued 0.55; one such session 60 us, 0.58 PFLOP/s: its 544 workgroups are 2.1 for each compute unit, where some have 3.
 // Stages of rows two or three ahead (61 and 80 us), two groups of wavefronts that take turns with the rows (70), 64 positions to a wavefront
-// (83), products among the exponentials of those before (59) and workgroups of 64 or 96 positions (152, 69) do not change that.
+// (83), 64 rows' scores at once where all rows see all positions (62), products among the exponentials of those before (59) and workgroups
+// of 64 or 96 positions (152, 69) do not change that.
 #include <atomic>
 #include <type_traits>
 
