@@ -841,7 +841,7 @@ int plc_pages_evict(const plc_pages *pages /* host */, const int32_t *keep, int3
  *   ids      the k largest logits' tokens, the largest first, of equal ones the lowest token first;
  *   top_logprobs, probs   y - lse and exp(y - lse) of those: `probs` is what plc_predict_residual takes;
  *   chosen   the token's place among them, or -1: what plc_predict_residual_cond takes.
- * Logits may be minus infinity (masked tokens).  A row with a NaN or plus infinity, or nothing but minus infinity, raises
+ * Logits may have any finite size, or be minus infinity (masked tokens).  A row with a NaN or plus infinity, or nothing but minus infinity, raises
  * status PLC_ERR_INVALID; its results are NaN, and ids and chosen -1.  A token that is none raises it too: logprob NaN,
  * chosen -1.  All sums in fp32.
  *   type     PLC_FP16, PLC_BF16 or PLC_FP32, of the logits.  Rows at `row_stride` elements, aligned as their elements are.

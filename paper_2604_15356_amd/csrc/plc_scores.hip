@@ -3,7 +3,10 @@
 //
 // A thread goes through the row's 16-byte pieces in steps of the workgroup and keeps a running maximum m, Z = sum 2^a and
 // T = sum a 2^a, a = c x - c m with c = scale * log2(e): then lse = ln 2 (c m + log2 Z) and the entropy is ln 2 (log2 Z - T / Z).
-// c m is rounded once, and the same number is taken from every c x by a fused product, so that its rounding drops out.
+// c m is rounded once, and the same number is taken from every c x by a fused product, so that its rounding drops out: below 2^24 it
+// is half a unit at most, and no weight is above sqrt 2.  Beyond that it would take weights out of range (at -1e10, a mask's value, it is
+// hundreds), so a maximum starts at -2^24: what lies far below weighs nothing, and where the whole row's lies beyond
+// it on either side, the row is gone through again with a = c (x - its largest).
 //
 // The k largest: call what each of 64 fours of threads has seen a group.  The group with the k-th largest maximum bounds the k
 // largest from below: at least k logits are as large.  What is not below it goes into a list in LDS: a thread looks its pieces through
@@ -26,8 +29,8 @@ namespace plc {
 namespace {
 
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
-constexpr float kNothing = -1e30f;  // c m before anything was seen; beyond +-it c x may overflow, and the row is gone through again
-constexpr float kGone = -200.0f;    // 2^kGone is zero
+constexpr float kNothing = -0x1p24f;  // c m before anything was seen; from +-it on fp32 has no fractions, and the row is gone through again
+constexpr float kGone = -200.0f;      // 2^kGone is zero
 constexpr int kGroups = 64, kMostK = 32, kMostParts = 32;
 constexpr int64_t kPartRows = 512;  // workgroups that rows are cut into parts for
 constexpr int64_t kLongRow = 8192;  // pieces of a row that is
@@ -46,7 +49,8 @@ struct ScoreArgs {
   uint32_t *status;
 };
 
-// Of a row, or of a part: the largest logit; Z and T of a = c (x - base) - shift.  base is zero but where c x could overflow.
+// Of a row, or of a part: the largest logit; Z and T of a = c (x - base) - shift.  base is zero but where the largest c x is 2^24 or more, or
+// -2^24 or less.
 struct Stats {
   float best, base, shift, z, t;
 };
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(kBlock) void score_kernel(ScoreArgs a) {
     for (int w = 1; w < kWaves; ++w) s.best = fmaxf(s.best, meet[0][w]);
     s.shift = s.best * a.scale2;
     const bool finite = fabsf(s.best) < __builtin_inff();
-    if (finite && !(fabsf(s.shift) < -kNothing)) {  // out of range: once more, from the largest
+    if (finite && !(fabsf(s.shift) < -kNothing)) {  // once more, from the largest
       s.base = s.best, s.shift = 0.0f;
       z = t = 0.0f;
       for (int32_t j = q0 + (int32_t)threadIdx.x; j < q1; j += kBlock) {

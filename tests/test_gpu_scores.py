@@ -190,6 +190,101 @@ def test_logits_of_any_size(dtype, N, V):
     check(x, 32, torch.full((N,), V // 2 + 50, dtype=torch.int32, device=DEV))
 
 
+def check_far(logits, k, tokens, temperature=1.0):
+    """Valid rows of logits of any size: as check, with a definition that takes all differences from the row's largest logit, as 64 bits have
+    no fractions either at 1e16.  The tolerances are check's."""
+    N, V = logits.shape
+    scorer = TokenScorer(V, k)
+    got = scorer.score(logits, tokens, temperature=temperature)
+    scorer.check_status()
+    scale = float(torch.tensor(1.0 / temperature, dtype=torch.float32))
+    steps = V / (256 * (4 if logits.dtype == torch.float32 else 8)) + 40
+    logits, t = logits.double().cpu(), tokens.cpu().long()
+    top = logits.amax(1)
+    below = (logits - top[:, None]) * scale
+    norm = torch.logsumexp(below, 1)
+    logs, lse = below - norm[:, None], top * scale + norm
+    p = logs.exp()
+    away = torch.where(p > 0, -below, torch.zeros_like(below))
+    A, A2 = (p * away).sum(1), (p * away * away).sum(1)
+    entropy = norm + A
+    err = U * (4 * A + steps)
+    within = lambda a, b, tol: bool(((a.double().cpu() == b) | ((a.double().cpu() - b).abs() <= tol)).all())  # noqa: E731
+    assert within(got.lse, lse, err + U * 6 * (lse.abs() + top.abs() * scale))
+    assert within(got.entropy, entropy, U * (4 * A2 + (A + entropy + 1) * (steps + 8)))
+    want = torch.where(t >= 0, logs.gather(1, t.clamp(min=0)[:, None])[:, 0], torch.zeros_like(top))
+    assert within(got.logprob, want, err + U * (6 * want.abs() + 8)) and bool((got.logprob.cpu()[t < 0] == 0).all())
+    if k:
+        ids = torch.sort(logits, dim=1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(got.ids.cpu().long(), ids)
+        want = torch.gather(logs, 1, ids)
+        assert within(got.logprobs, want, err[:, None] + U * (6 * want.abs() + 8))
+        assert within(got.probs, want.exp(), want.exp() * (err[:, None] + U * (12 * want.abs() + 16)) + 1e-37)
+        hit = ids == t[:, None]
+        assert torch.equal(got.chosen.cpu().long(), torch.where(hit.any(1), hit.int().argmax(1), torch.tensor(-1)))
+
+
+def rows_with_masks(V, dtype, value, seed):
+    """Rows in which tokens are masked by a finite value: all but a few, whole runs in front, behind or up to the last token; and rows of nothing but
+    such values, of one size and of several, of both signs."""
+    gen = torch.Generator(DEV).manual_seed(seed)
+    x = torch.randn((9, V), device=DEV, generator=gen) * 3
+    few = torch.randint(0, V, (7,), device=DEV, generator=gen)
+    x[0] = torch.full_like(x[0], value).scatter(0, few, x[0][few])
+    x[1, :2 * V // 3] = value
+    x[2, V // 3:] = value
+    x[3, :V - 1] = value
+    x[4], x[5] = value, -value
+    x[6:8] = torch.rand((2, V), device=DEV, generator=gen) + 0.5
+    x[6] *= value
+    x[7] *= -value
+    x[8] = torch.where(torch.arange(V, device=DEV) < V // 2, value, 2 * value)
+    return x.to(dtype)
+
+
+MASKS = {torch.float16: ((-3e4, -2e4, -1e3), (1e-3, 1e-4, 1e-6)),
+         torch.bfloat16: ((-1e7, -1e8, -1e9, -1e10, -1e15, -1e20, -1e29), (1.0, 0.7, 0.1)),
+         torch.float32: ((-1e7, -1e8, -1e9, -1e10, -1e15, -1e20, -1e29), (1.0, 0.7, 0.1))}
+
+
+@TYPES
+@pytest.mark.parametrize("which", range(3))
+@pytest.mark.parametrize("N,V", [(2, 100), (2, 3000), (2, 9001), (2, 140000), (600, 9001)])
+def test_finite_values_that_mask(dtype, which, N, V):
+    """Where fp32 does not hold the fractions of what a row is scaled to; such rows are valid (check_far looks at the status)."""
+    values, temperatures = MASKS[dtype]
+    x = torch.cat([rows_with_masks(V, dtype, value, i) for i, value in enumerate(values)])
+    tokens = x.float().argmax(1).to(torch.int32)
+    tokens[1::3] = V // 2
+    tokens[2::5] = -1
+    if N > len(x):
+        at = torch.arange(N, device=DEV) % len(x)
+        for k in (0, 32):
+            check_far(x[at].contiguous(), k, tokens[at], temperature=temperatures[which])
+        return
+    for i in range(0, len(x) - 1, 2):
+        check_far(x[i:i + 2], (32, 0, 8)[i // 2 % 3], tokens[i:i + 2], temperature=temperatures[which])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,V", [(2, 3000), (2, 140000), (600, 9001)])
+def test_logits_about_the_size_that_a_row_is_gone_through_again_from(dtype, N, V):
+    """2^24 over log2(e), 11,629,000: a little below and above, all of a row and a run of it (of which parts have one, or two), of both signs."""
+    for i, size in enumerate((1.1e7, 1.16e7, 1.1629e7, 1.163e7, 1.2e7, 1.3e7)):
+        x, tokens = draw(N, V, torch.float32, seed=i)
+        x[0::4] += size
+        x[1::4] -= size
+        x[2::4, V // 2:] += size
+        x[3::4, :V // 2] -= size
+        if N == 2:
+            x = torch.cat([x, draw(N, V, torch.float32, seed=i + 10)[0]])
+            x[2, V // 2:] += size
+            x[3, :V // 2] -= size
+        x = x.to(dtype)
+        for a in range(0, len(x), N):
+            check_far(x[a:a + N], (0, 20, 32)[i % 3], tokens)
+
+
 @TYPES
 def test_rows_and_tokens_that_are_none(dtype):
     for N in (4, 700):
