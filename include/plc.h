@@ -803,8 +803,8 @@ typedef struct plc_weights {
  *   weights[s, layer, h, p]  =  decay * weights[s, layer, h, p] + sum_p   for p < c,  sum_p  for c <= p < lens[s].
  * (Of a drafted tree the accepted nodes alone count: after plc_pages_accept they are a chain, with their rows of q and lse.)
  * With decay = 0 what weights hold is not read.  Positions that a row does not see take nothing from it, whatever they
- * hold.  Products of 16-bit values accumulated in fp32, all else fp32.  The order of the sums is fixed.  Sessions without nodes
- * take no part.
+ * hold.  Products of 16-bit values accumulated in fp32, all else fp32.  The order of a session's sums is fixed, whatever else is in
+ * the call and whatever bounds it has.  Sessions without nodes take no part.
  *   layer, type, q, q_stride, G, N, off, max_nodes, max_len, scale: as for plc_attend, with its limits; S * H < 2^23.
  *   lse      fp32 [N, H*G], as plc_attend leaves it.
  *   decay    0..1.

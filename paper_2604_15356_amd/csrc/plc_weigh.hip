@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 ? 2 : 1) void weigh_few_kernel(We
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) sc = mfma<T>(qf[ks], kf[n & 1][ks], sc);
       const int32_t pos = first + 32 * n + col, my_first = max(0, pos - ctx) * a.G;  // the first row that sees it
-      float sum = 0.0f;
+      float part[2] = {0.0f, 0.0f};  // (in the order that the kernel of many rows has: a session's bits are its own, whatever bounds the call has)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         if (8 * g < R) {
@@ -157,10 +157,11 @@ __global__ __launch_bounds__(kBlock, DP <= 128 ? 2 : 1) void weigh_few_kernel(We
           for (int b = 0; b < 4; ++b) {
             const int r = 8 * g + 4 * half + b;
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * g + b], a.scale2, -lse2[4 * g + b]));
-            sum += r < R && r >= my_first ? w : 0.0f;
+            part[b & 1] += r < R && r >= my_first ? w : 0.0f;
           }
         }
       }
+      float sum = part[0] + part[1];
       sum += __shfl_xor(sum, 32);
       if (pos < v.len && half == 0) {
         if (p.page_ok(page[n])) put_weight(a, weights + pos, pos < ctx, before[n & 1], sum);

@@ -176,7 +176,8 @@ class PagedKVCache:
     def add_weights(self, q, off, lse, weights, decay=1.0, layer=0, scale=None, max_nodes=None, max_len=None):
         """Adds to weights (make_weights) what `layer`'s positions receive from the sessions' last off[s+1] - off[s] positions, a
         chain: q [N, H*G, d] and lse [N, H*G] as for attend and from it, so many times what was there before (`decay`; the call's own
-        positions begin with nothing).  Of a drafted tree only what was accepted counts: call it after `accept`, with those rows."""
+        positions begin with nothing).  Of a drafted tree only what was accepted counts: call it after `accept`, with those rows.
+        max_nodes, max_len as for attend; of single tokens of many sessions max_nodes=1 is worth saying, as N sets the launch without."""
         if q.dim() != 3 or q.dtype is not self.dtype:
             raise ValueError(f"q is [nodes, heads, d] of {self.dtype}")
         N = q.shape[0]

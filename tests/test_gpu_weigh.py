@@ -163,6 +163,28 @@ def test_the_same_bits_every_time_and_whatever_else_is_in_the_call():
     assert torch.equal(weights[0][0], weights[3][0])
 
 
+@BOTH
+@pytest.mark.parametrize("d", [40, 64, 80, 128, 256])
+@pytest.mark.parametrize("G,t", [(1, 1), (1, 9), (4, 1), (4, 8), (3, 10), (5, 6), (32, 1), (1, 32)])
+def test_a_session_s_bits_whatever_bounds_the_call_has(dtype, d, G, t):
+    """Up to 32 rows of a session are added in the same order in a call for few rows and in one for many: what decides between them (max_nodes,
+    by default the rows of all sessions) does not show."""
+    lens, counts = [300, 129, t], [t, max(1, t - 1), t]
+    cache, _ = make_cache(dtype, d, 2, 16, lens, seed=t)
+    q = (2 * torch.randn((sum(counts), 2 * G, d), device=DEV)).to(dtype)
+    off = offsets(counts)
+    _, lse = cache.attend(q, off)
+    start = torch.rand(cache.make_weights().shape, device=DEV)
+    results = []
+    for most in (t, 32 // G + 1, 1000):
+        weights = start.clone()
+        cache.add_weights(q, off, lse, weights, decay=0.75, max_nodes=most, max_len=300)
+        results.append(weights)
+    cache.check_status()
+    assert t * G <= 32 < (32 // G + 1) * G
+    assert torch.equal(results[0], results[1]) and torch.equal(results[0], results[2])
+
+
 def test_sessions_that_are_not_as_described():
     """Status, and their weights as they were; the others' as ever."""
     lens, counts = [50, 60, 40], [2, 3, 2]
