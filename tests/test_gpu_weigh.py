@@ -185,6 +185,30 @@ def test_a_session_s_bits_whatever_bounds_the_call_has(dtype, d, G, t):
     assert torch.equal(results[0], results[1]) and torch.equal(results[0], results[2])
 
 
+@pytest.mark.parametrize("d,counts", [(64, {0: 1, 5: 3}), (72, {0: 2, 5: 1}), (200, {0: 1, 5: 2}),
+                                      (64, {0: 100, 5: 130}), (40, {0: 70, 5: 64}), (128, {0: 33, 5: 129}), (200, {0: 64, 5: 40})])
+def test_more_positions_than_the_workgroups_take_at_once(d, counts):
+    """4096 sessions and heads: a workgroup takes 16 times its 128, or few rows 512 (d > 128: 256), positions and more of the long sessions, one lot after the
+    other; of few rows and of many, of which the lots have one stage, or two, or three."""
+    S, H = 64, 64
+    lens = [9500 if s == 0 else 5000 if s == 5 else 40 + s for s in range(S)]
+    counts = [counts.get(s, 1) for s in range(S)]
+    cache, (k, _) = make_cache(torch.float16, d, H, 16, lens, seed=d)
+    q = torch.randn((sum(counts), H, d), device=DEV).to(torch.float16)
+    off, bounds = offsets(counts), dict(max_nodes=max(counts), max_len=9500)
+    _, lse = cache.attend(q, off, **bounds)
+    weights = torch.rand((S, 1, H, cache.M * 16), device=DEV)
+    before = weights.clone()
+    cache.add_weights(q, off, lse, weights, decay=0.5, **bounds)
+    cache.check_status()
+    heads = [0, 31, 63]
+    want, tol = definition(q[:, heads], k[:, 0, heads], lse[:, heads], lens, counts, 1, d ** -0.5, before[:, 0, heads], 0.5)
+    for s, n in enumerate(lens):
+        got = weights[s, 0, heads].double().cpu()
+        assert bool(((got[:, :n] - want[s, :, :n]).abs() <= tol[s, :, :n]).all()), s
+        assert torch.equal(weights[s, 0, :, n:], before[s, 0, :, n:])
+
+
 def test_sessions_that_are_not_as_described():
     """Status, and their weights as they were; the others' as ever."""
     lens, counts = [50, 60, 40], [2, 3, 2]
