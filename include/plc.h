@@ -791,6 +791,11 @@ int plc_rotate_store(const plc_pages *pages /* host */, const plc_rows *rows /* 
  *   weights   fp32, logical [S, L, H, width] through `stride` (of session, layer, head; positions are contiguous): what
  *             position p of a session has received in a layer and KV head.  16-byte aligned; strides and width multiples of 4.
  *             No two lie on each other: in the order of their strides, each reaches past what those before it span.
+ *
+ * The weights are the caller's, and nobody tells them what becomes of a session.  What plc_attend_weights adds up for a position
+ * begins with its row only where that is among the last t of the call.  Rows that come otherwise (stored without the call, restored, forked from
+ * another session, in a session's place that was given to another) take over what is in their positions' places, which plc_pages_evict and
+ * plc_pages_trim leave there too: the caller puts 0 there first, or what the row has received elsewhere.
  */
 typedef struct plc_weights {
   float *w;

@@ -160,8 +160,10 @@ class PagedKVCache:
 
     # -- what positions have received, and eviction by it ---------------------------------------
     def make_weights(self):
-        """Zeros for all that positions receive: float32 [S, L, H, positions].  Sessions that are forked take theirs along by
-        weights.copy_(weights[src])."""
+        """Zeros for all that positions receive: float32 [S, L, H, positions].  They are the caller's, and nothing but add_weights and evict changes
+        them.  Sessions that are forked take theirs along by weights.copy_(weights[src]).  Where rows come to positions n0 and up without
+        add_weights (a prefix that is restored, a prompt of which only the last rows are counted, a session's place given to another), what others had received
+        there would count for them: weights[s, :, :, n0:] = 0 first."""
         return torch.zeros((self.S, self.L, self.H, self.M * self.B), dtype=torch.float32, device=self.device)
 
     def _weights(self, w):
@@ -176,7 +178,7 @@ class PagedKVCache:
     def add_weights(self, q, off, lse, weights, decay=1.0, layer=0, scale=None, max_nodes=None, max_len=None):
         """Adds to weights (make_weights) what `layer`'s positions receive from the sessions' last off[s+1] - off[s] positions, a
         chain: q [N, H*G, d] and lse [N, H*G] as for attend and from it, so many times what was there before (`decay`; the call's own
-        positions begin with nothing).  Of a drafted tree only what was accepted counts: call it after `accept`, with those rows.
+        positions begin with nothing, others with what is in their places: see make_weights).  Of a drafted tree only what was accepted counts: call it after `accept`, with those rows.
         max_nodes, max_len as for attend; of single tokens of many sessions max_nodes=1 is worth saying, as N sets the launch without."""
         if q.dim() != 3 or q.dtype is not self.dtype:
             raise ValueError(f"q is [nodes, heads, d] of {self.dtype}")

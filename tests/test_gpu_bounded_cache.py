@@ -149,3 +149,39 @@ def test_a_drafted_tree_s_accepted_nodes():
     # (the same scores, summed in another order)
     assert bool(((out - out2).abs() <= 2 * HALF * 1.1 * out2.abs() + 4 * HALF).all())
     assert bool(((lse - lse2).abs() < 1e-5).all()) and bool(((w - w2).abs() <= 4e-5 * w2 + 1e-6).all())
+
+
+def test_a_session_s_place_given_to_another():
+    """The weights of those before count for rows that come without add_weights, also behind what was evicted or trimmed; with zeros put there
+    first all is as in a cache of its own."""
+    torch.manual_seed(5)
+    prompt = [torch.randn((50, L, H, d), device=DEV).to(torch.float16) for _ in range(2)]
+    new = [torch.randn((2, L, H, d), device=DEV).to(torch.float16) for _ in range(2)]
+    q = torch.randn((2, H * G, d), device=DEV).to(torch.float16)
+
+    def conversation(cache, weights):
+        cache.extend(ints([50]))
+        cache.store(*prompt, ints([0, 50]))
+        cache.extend(ints([2]))
+        cache.store(*new, ints([0, 2]))
+        for layer in range(L):
+            _, lse = cache.attend(q, ints([0, 2]), layer=layer)
+            cache.add_weights(q, ints([0, 2]), lse, weights, layer=layer)
+        return weights.clone(), cache.evict(ints([20]), weights, first=1, last=3)[..., :20].clone()
+
+    caches = [PagedKVCache.create(8, L, H, d, 1, 64, B=B) for _ in range(3)]
+    weights = [cache.make_weights() for cache in caches]
+    for cache, w in zip(caches[1:], weights[1:]):  # another conversation had this place, and was shortened in both ways
+        cache.extend(ints([60]))
+        cache.store(*(torch.randn((60, L, H, d), device=DEV).to(torch.float16) for _ in range(2)), ints([0, 60]))
+        w.copy_(torch.rand(w.shape, device=DEV) * 5)
+        cache.evict(ints([30]), w, first=1, last=3)
+        cache.trim(ints([0]))
+    before = weights[2].clone()
+    weights[1][0, :, :, 0:] = 0
+    (own, kept), (reused, kept2), (stale, _) = (conversation(*x) for x in zip(caches, weights))
+    for cache in caches:
+        cache.check_status()
+    assert torch.equal(own[..., :52], reused[..., :52]) and torch.equal(kept, kept2)
+    want = own.double()[..., :50] + before.double()[..., :50]
+    assert bool(((stale.double()[..., :50] - want).abs() <= 2.0 ** -23 * want).all()) and torch.equal(stale[..., 50:52], own[..., 50:52])
