@@ -810,8 +810,8 @@ typedef struct plc_weights {
  * With decay = 0 what weights hold is not read.  Positions that a row does not see take nothing from it, whatever they
  * hold.  Products of 16-bit values accumulated in fp32, all else fp32.  The order of a session's sums is fixed, whatever else is in
  * the call and whatever bounds it has.  Sessions without nodes take no part.
- *   layer, type, q, q_stride, G, N, off, max_nodes, max_len, scale: as for plc_attend, with its limits; S * H < 2^23.
- *   lse      fp32 [N, H*G], as plc_attend leaves it.
+ *   layer, type, q, q_stride, G, N, off, max_nodes, max_len, scale: as for plc_attend, with its limits; S * H < 2^23; scale * log2(e) is finite.
+ *   lse      fp32 [N, H*G], as plc_attend leaves it.  A row's weights are as exact as this is: some 2^-22 of its size, relatively (2 % at 10^5).
  *   decay    0..1.
  * Where a page is none, PLC_ERR_INVALID is raised and positions on it are left alone; where a session's numbers are not as described
  * (or it has more than `width` positions), all of its weights. */

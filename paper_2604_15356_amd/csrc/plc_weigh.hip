@@ -395,7 +395,7 @@ extern "C" int plc_attend_weights(const plc_pages *pages, int32_t layer, int32_t
   if (!pages_valid(pages) || pages->d > 256 || layer < 0 || layer >= pages->L || (type != PLC_FP16 && type != PLC_BF16) ||
       !q_stride || q_stride[0] < 0 || q_stride[0] % 8 || q_stride[1] < 0 || q_stride[1] % 8 || G < 1 || N < 0 || N > INT32_MAX ||
       (int64_t)pages->H * G > 65536 || max_nodes < 1 || (int64_t)max_nodes * G > INT32_MAX / 256 || max_len < 1 ||
-      !aligned(off, 4) || !(scale > 0.0f) || !(scale < __builtin_inff()) || !(decay >= 0.0f) || !(decay <= 1.0f) ||
+      !aligned(off, 4) || !(scale > 0.0f) || !(scale * kLog2e < __builtin_inff()) || !(decay >= 0.0f) || !(decay <= 1.0f) ||
       !weights_valid(pages, weights) || !status)
     return PLC_ERR_INVALID;
   if ((int64_t)pages->S * pages->H >= 1 << 23) return PLC_ERR_INVALID;  // (lanes of a launch < 2^32)

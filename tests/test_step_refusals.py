@@ -125,6 +125,11 @@ def test_weighings_that_are_refused(over):
     assert weigh(**over) == INVALID
 
 
+def test_scales_beyond_what_their_product_with_log2_e_holds_are_refused():
+    """Of a score of 0 and an infinite scale a weight would be NaN."""
+    assert weigh(scale=2.4e38) == INVALID and weigh(N=0, q=None, lse=None, scale=2.3e38) == plc.PLC_OK
+
+
 # Each stride for itself is as large as what it steps over, and together they meet.
 @pytest.mark.parametrize("over", [dict(stride0=128, stride1=128), dict(stride0=64, stride1=192), dict(stride0=128, stride1=256, stride2=256),
                                   dict(stride0=192, stride1=128), dict(stride0=1 << 62, stride1=64)])
