@@ -185,3 +185,42 @@ def test_a_session_s_place_given_to_another():
     assert torch.equal(own[..., :52], reused[..., :52]) and torch.equal(kept, kept2)
     want = own.double()[..., :50] + before.double()[..., :50]
     assert bool(((stale.double()[..., :50] - want).abs() <= 2.0 ** -23 * want).all()) and torch.equal(stale[..., 50:52], own[..., 50:52])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_a_thinned_cache_back_to_the_coder_and_into_pages_again(interleaved):
+    """After an eviction a row is another position in each layer and head: rotate takes them one by one."""
+    torch.manual_seed(11)
+    rotary, n, now = Rotary(d, base=1000.0, interleaved=interleaved), 60, 23
+    cache = PagedKVCache.create(8, L, H, d, 1, 64, B=B)
+    weights = cache.make_weights()
+    k, v = (torch.randn((n, L, H, d), device=DEV).to(torch.float16) for _ in range(2))
+    cache.extend(ints([n]))
+    cache.store_rotated(k, v, ints([0, n]), rotary)
+    weights.copy_(torch.rand(weights.shape, device=DEV))
+    kept = cache.evict(ints([now]), weights, first=1, last=3)[0, :, :, :now].permute(2, 0, 1).contiguous()  # [now, L, H]
+    rows = [torch.empty((now, L, H, d), dtype=torch.float16, device=DEV) for _ in range(2)]
+    cache.load(*rows, ints([0, now]))
+    cache.check_status()
+    each = lambda x: x.reshape(-1, 1, d)  # noqa: E731
+    positions = kept.flatten()
+    at = kept.long()[..., None].expand(now, L, H, d)
+    before, values = torch.gather(k, 0, at), torch.gather(v, 0, at)
+    assert torch.equal(rows[1], values) and torch.equal(rotary.rotate(each(before), positions), each(rows[0]))
+    back = rotary.rotate(each(rows[0]), positions, inverse=True).view(now, L, H, d)
+    # stored rows are off by half a step each, of which the inverse turns two together; then half a step of its own; sines and products far below
+    x = before.double()
+    size = torch.cat([x[..., : d // 2].abs() + x[..., d // 2:].abs()] * 2, -1) if not interleaved else \
+        (x[..., ::2].abs() + x[..., 1::2].abs()).repeat_interleave(2, -1)
+    assert bool(((back.double() - x).abs() <= 2.001 * HALF * size + 1.001 * HALF * x.abs() + 2.0 ** -24).all())
+    other = PagedKVCache.create(8, L, H, d, 1, 64, B=B)
+    other.extend(ints([now]))
+    other.store(rotary.rotate(each(before), positions).view(now, L, H, d), values, ints([0, now]))
+    q = torch.randn((1, H * G, d), device=DEV).to(torch.float16)
+    outs = []
+    for c in (cache, other):  # the next token of either: after what the session has seen
+        c.extend(ints([1]))
+        turned = c.store_rotated(k[:1], v[:1], ints([0, 1]), rotary, q=q, base=ints([n]))
+        outs.append(c.attend(turned, ints([0, 1]), layer=1)[0])
+        c.check_status()
+    assert torch.equal(*outs)

@@ -215,6 +215,23 @@ def test_many_rows_past_the_caches(L, n):
     assert same_bits(got_k.reshape(n, L * H, d), want) and same_bits(got_v, v[0].permute(2, 0, 1, 3))
 
 
+@pytest.mark.parametrize("d,r", [(96, 24), (80, 20), (72, 18)])
+def test_many_rows_in_halves_of_other_widths(d, r):
+    """Halves of 8, 4 and 2 bytes' alignment, more than 96 MB: as a hundred rows at a time."""
+    L, H, n = 8, 8, 4001
+    cache, _ = make_cache(torch.float16, d, H, 16, [n], seed=1, L=L)
+    k, v = (torch.randn((n, L, H, d), device=DEV, dtype=torch.float16) for _ in range(2))
+    rotary = Rotary(d, r=r)
+    cache.store_rotated(k, v, offsets([n]), rotary)
+    cache.check_status()
+    x = k.view(n, L * H, d)
+    positions = torch.arange(n, device=DEV, dtype=torch.int32)
+    want = torch.cat([rotary.rotate(x[a:a + 100], positions[a:a + 100]) for a in range(0, n, 100)])
+    got_k, got_v = rows_of(cache, 0)
+    assert 8 * x.numel() > 96 << 20 and same_bits(got_k.reshape(n, L * H, d), want) and same_bits(got_v, v)
+    assert same_bits(rotary.rotate(x, positions), want)
+
+
 def test_pages_that_cannot_be_stored_to():
     """Rows on shared pages, or on none, are left alone, with their queries; the others are stored."""
     cache, _ = make_cache(torch.float16, 64, 2, 16, [20, 40, 18], seed=3, fill=1.0)
