@@ -11,8 +11,8 @@
 // of some numbers before it writes any of them needs to look at no other order: what later numbers read lies behind it.
 //
 // What bounds it: HBM for the rows, read once and written once (4 sessions of 2048 positions halved in 32 layers of 8 heads, 128
-// components: 1.09 GB in 232 us, 4.7 TB/s; a copy of such a size 5.4); for few the steps of the choice, one behind the other
-// (7 us for 512 positions, before their rows move).
+// components: 1.09 GB in 232 us, 4.7 TB/s; a copy of such a size 5.4), which wait while all workgroups choose (14 us of it); for few the steps of
+// the choice, one behind the other (7 us for 512 positions, before their rows move).
 #include "plc_device.h"
 #include "plc_paged.h"
 
@@ -295,14 +295,19 @@ extern "C" int plc_pages_evict(const plc_pages *pages, const int32_t *keep, int3
   const int64_t heads = (int64_t)a.p.L * a.p.H;
   if (heads >= 1 << 22 || heads * pages->d >= 1 << 29) return PLC_ERR_INVALID;  // (lanes of a launch < 2^32)
   const dim3 grid((unsigned)heads, (unsigned)a.p.S);
-  // Where there are sessions and heads enough for all compute units, or little to move, a workgroup moves what it has chosen, whole rows at a
-  // time; else K and V and their lines of 128 bytes have workgroups of their own.  (32 layers and 8 heads, 128 components, halved: 64 sessions of 200
-  // positions 337 against 389 us, a session of 8000 228 against 235; of 8 layers, 4 sessions of 2000 65 against 70; of 4, 53 against 42.)
+  // Where there are sessions and heads enough for all compute units, or little that may have to be moved (W rows: the host knows no more), a workgroup
+  // moves what it has chosen, whole rows at a time; else K and V and their lines of 128 bytes have workgroups of their own.  (32 layers and 8 heads, 128 components, halved: 64 sessions of 200
+  // positions 337 against 389 us, a session of 8000 228 against 235; of 8 layers, 4 sessions of 2000 65 against 70; of 4, 53 against 42.  Little:
+  // in a graph, 8 heads of 64 components, 64 rows that stay 14.3 against 14.8 us, 512 18.5 against 17.7, 768 22.4 against 20.1; the launch that is saved
+  // takes 3.3 of the host's.)
   const int64_t rows = heads * a.p.S;
   const bool together = rows >= kComputeUnits || (int64_t)W * a.p.d8 <= kLittle;
   const bool past = (double)rows * W * a.p.d8 * 64 > (double)kCached;  // of both halves, in and out
   a.pieces = a.p.d8 > kBlock ? kBlock : !together && a.p.d8 % 8 == 0 ? 8 : a.p.d8;
   a.columns = (a.p.d8 + a.pieces - 1) / a.pieces;
+  // Four wavefronts up to the 4096 positions that they hold in registers, 16 beyond (a pass with a head's rows, us, of 256 and of 1024 threads: one head,
+  // 1000 positions 17.0 and 18.0, 4096 28.8 and 27.5, 6000 40.5 and 35.5, 32,000 151 and 129; 1024 heads of 64 components, 500 positions 44 and 73,
+  // 1000 71 and 88, 4000 245 and 244, 8000 483 and 464).
   const auto chosen = max_len <= 4096 ? (!together ? &select_kernel<256, 0> : past ? &select_kernel<256, 2> : &select_kernel<256, 1>)
                                       : (!together ? &select_kernel<1024, 0> : past ? &select_kernel<1024, 2> : &select_kernel<1024, 1>);
   hipLaunchKernelGGL(chosen, grid, dim3(max_len <= 4096 ? 256 : 1024), 0, st, a);

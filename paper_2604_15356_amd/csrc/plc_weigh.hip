@@ -10,7 +10,7 @@
 // What bounds it: few rows, HBM (64 sessions' tokens, 8 heads of 4, 128 components: after 4096 positions each 537 MB in 116 us, 4.6 TB/s; after
 // up to 4096 273 MB in 64 us; staged through LDS the first took 113, past the caches 164).  Many rows, the turns of the matrix cores and the
 // vector units: 32 x 32 scores of 128 components take 256 cycles of products, and some 64 vector instructions, 16 of them exponentials.  8
-// sessions of 512 tokens after 8192 positions 335 us, 0.84 PFLOP/s, where the matrix cores are busy 0.39 of the time and vector instructions
+// sessions of 512 tokens after 8192 positions 334 us, 0.84 PFLOP/s, where the matrix cores are busy 0.39 of the time and vector instructions
 // are issued 0.55; one such session 60 us, 0.58 PFLOP/s: its 544 workgroups are 2.1 for each compute unit, where some have 3.
 // Stages of rows two or three ahead (61 and 80 us), two groups of wavefronts that take turns with the rows (70), 64 positions to a wavefront
 // (83), 64 rows' scores at once where all rows see all positions (62), products among the exponentials of those before (59) and workgroups
@@ -180,8 +180,9 @@ struct ManyShape {
   static constexpr size_t kLds = 2 * (size_t)(kStage + kRows * 4);
 };
 
-// Four wavefronts a SIMD where their registers allow it: 16 sessions, 8 heads of 8, 16 nodes after 3000 positions 35.0 us, with
-// three 38.7; 512 nodes after 8192 63 and 60 us.
+// Four wavefronts a SIMD, though at 128 components 8 to 10 registers are kept in scratch for it, outside of the loops: 8 sessions, 8 heads of 4, 512
+// nodes after 8192 positions 334 us, with three 340; 5 sessions of up to 27 nodes and 4095 positions 12.0 and 12.6; as good as the same: one session of
+// 512 nodes after 8192 (61 and 60.5 us), 2048 after 8192 (222), 16 sessions, 8 heads of 8, 16 nodes after 3000 (30.7).
 template <class T, int DP, bool kExact>
 __global__ __launch_bounds__(kBlock, DP <= 128 ? 4 : 2) void weigh_many_kernel(WeighArgs a) {
   using Shape = ManyShape<DP>;

@@ -194,7 +194,7 @@ class PagedKVCache:
     def evict(self, keep, weights, kept=None, first=0, last=0, max_len=None):
         """Every session of more than keep[s] positions (int32 [S]) is shortened to that, in each layer and head to its first and
         last positions and those with the largest weights, which move along.  Returns kept, int32 [S, L, H, W]: the positions
-        that stayed, in front; W is at least what a session has afterwards (default: max_len).  The pages from position `first` on have to be
+        that stayed, in front; W is at least what a session has afterwards (default: max_len), and the launch goes by it.  The pages from position `first` on have to be
         the sessions' own: what others share can stay as the first positions.  A row is another position in each layer and head then (store_rotated
         has one for all): what `load` gives goes back to where it was rotated from, and there again, as rows of one head, rotary.rotate(k.view(-1, 1, d),
         positions), by the positions that `kept` names.  max_len: no session has more (default: what the table holds)."""
